@@ -268,6 +268,64 @@ xq_status xq_mx_gemm_staged(int32_t M, const xq_mx_weights* w, void* out_bf16_de
 xq_status xq_mx_expanded_linear_host(const void* X_bf16_host, int32_t M, const xq_mx_weights* w, void* out_bf16_host,
                                      void* ws_dev, size_t ws_bytes, void* stream);
 
+/* 8-bit floating-point layer (no counterpart in the paper: it is for the linears that stay unexpanded, and for the norm and
+ * the gated activation around the expanded ones).
+ *
+ * Format: E4M3 elements with one E8M0 scale byte b, the power of two 2^(b - 127), for each group of 128 consecutive channels
+ * of a token row and for each 128 x 128 block of a weight matrix.  For a group with a = max |v| (NaN left out):
+ *   e = the smallest integer with a <= 448 * 2^e, at least -127 (0 for a group of zeros);  b = e + 127;
+ *   code = the E4M3 value nearest to v / 2^e, ties to even (NaN stays NaN; an infinity makes its group's scale 2^120, where the
+ *   largest element stands for 448 * 2^120, above the fp32 range).
+ * Token rows, wherever they cross this boundary: codes dev [M, Kq] bytes, Kq = K rounded up to 128 (padding: zero codes), and
+ * scales dev [M, P] bytes, P = ceil(K / 128) rounded up to 4 (padding bytes: 127).  codes 16-byte aligned, scales 4-byte.
+ * Any K >= 1 and N >= 1.  M = 0 is a no-op.  Products accumulate in fp32 and are rounded once at the end.
+ *
+ * xq_f8_weights is opaque (device memory owned by the library).  xq_f8_prepare_weights quantizes bf16 weights [N, K];
+ * xq_f8_weights_import takes codes [N, K] (E4M3 bytes) and scales [ceil(N / 128), ceil(K / 128)]; 255, the NaN scale, is
+ * refused (INVALID_ARG).  Both take HOST or DEVICE memory, run on `stream` and synchronize it.  xq_f8_weights_export writes the
+ * canonical form back to the HOST and synchronizes.  N and K at most 2^24. */
+typedef struct xq_f8_weights xq_f8_weights;
+xq_status xq_f8_prepare_weights(const void* W_bf16, int32_t N, int32_t K, void* stream, xq_f8_weights** out);
+xq_status xq_f8_weights_import(const uint8_t* codes, const uint8_t* scales, int32_t N, int32_t K, void* stream, xq_f8_weights** out);
+xq_status xq_f8_weights_export(const xq_f8_weights* w, uint8_t* codes_host, uint8_t* scales_host);
+xq_status xq_f8_weights_info(const xq_f8_weights* w, int32_t* N, int32_t* K);
+void xq_f8_weights_free(xq_f8_weights* w);
+
+/* Token rows to 8 bits.  X bf16 dev, row pitch ldx elements (>= K, a multiple of 8).  K at most 65536. */
+xq_status xq_f8_quant(const void* X_bf16_dev, int32_t M, int32_t K, int64_t ldx, uint8_t* codes_dev, uint8_t* scales_dev, void* stream);
+
+/* Residual addition, RMS norm and quantization in one pass over the rows:
+ *   t = x + residual (t = x without one);  sum = bf16(t);  y = t / sqrt(mean(t^2) + eps) * gamma;  codes, scales = y in 8 bits.
+ * t and y stay in fp32 in between (t is not rounded to bf16 before the norm).  residual_opt and sum_opt share the pitch ldr and
+ * may be the same array (the residual stream updated in place); either may be NULL.  Y_opt, if not NULL, also receives
+ * bf16(y) at pitch ldy, for a consumer that takes bf16 tokens (xq_expanded_linear).  gamma bf16 dev [K].  Pitches: >= K and
+ * multiples of 8; all bf16 pointers 16-byte aligned; eps >= 0.  K at most 65536.  Elements between K and the pitch are neither
+ * read nor written. */
+xq_status xq_f8_norm_quant(const void* X_bf16_dev, int32_t M, int32_t K, int64_t ldx, const void* residual_bf16_opt_dev, int64_t ldr,
+                           const void* gamma_bf16_dev, float eps, void* sum_bf16_opt_dev, uint8_t* codes_dev, uint8_t* scales_dev,
+                           void* Y_bf16_opt_dev, int64_t ldy, void* stream);
+
+/* Bytes of device workspace that xq_f8_linear needs for up to M_max tokens; xq_f8_gemm and xq_f8_gated need its first 256 only
+ * (the status word).  Initialise once with xq_workspace_init; status through xq_poll_status.  Concurrent calls need distinct
+ * workspaces. */
+size_t xq_f8_workspace_bytes(int32_t M_max, const xq_f8_weights* w);
+
+/* out[m][n] = bf16( sum over groups g of 2^(e_x[m][g] + e_w[n / 128][g]) * sum over k in g of x[m][k] w[n][k] ), out dev bf16
+ * [M, N] row-major, 16-byte aligned.  xq_f8_linear is xq_f8_quant and xq_f8_gemm on `stream`, the 8-bit tokens staying in the
+ * workspace (K at most 65536). */
+xq_status xq_f8_gemm(const uint8_t* codes_dev, const uint8_t* scales_dev, int32_t M, const xq_f8_weights* w, void* out_bf16_dev, void* ws_dev,
+                     size_t ws_bytes, void* stream);
+xq_status xq_f8_linear(const void* X_bf16_dev, int32_t M, int64_t ldx, const xq_f8_weights* w, void* out_bf16_dev, void* ws_dev,
+                       size_t ws_bytes, void* stream);
+
+/* The gated pair of products of a feed-forward block in one kernel: with G and U the products of the tokens with `gate` and `up`
+ * (same N and K), h = G / (1 + exp(-G)) * U in fp32, and either out = bf16(h) [M, N] (what xq_expanded_linear takes as the
+ * tokens of an expanded down projection) or h in 8 bits, out_codes [M, N rounded up to 128] and out_scales (what xq_f8_gemm
+ * takes).  Exactly one of the two results is asked for; the other pointers are NULL. */
+xq_status xq_f8_gated(const uint8_t* codes_dev, const uint8_t* scales_dev, int32_t M, const xq_f8_weights* gate, const xq_f8_weights* up,
+                      void* out_bf16_opt_dev, uint8_t* out_codes_opt_dev, uint8_t* out_scales_opt_dev, void* ws_dev, size_t ws_bytes,
+                      void* stream);
+
 /* The whole layer on HOST buffers: copies X (host, [M, K] contiguous; pinned memory makes the
  * copies asynchronous) into the workspace, runs the layer, copies out (host, bf16 [M, N]) back
  * and synchronizes `stream` before returning. */

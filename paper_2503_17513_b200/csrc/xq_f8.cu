@@ -1,0 +1,369 @@
+// Entry points of the 8-bit floating-point layer: argument checks, weights objects, workspace.
+#include <string.h>
+
+#include <new>
+#include <vector>
+
+#include "xq_f8.h"
+#include "xq_internal.h"
+
+namespace {
+
+inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+constexpr int32_t kMaxRow = 65536;  // longest row the one-pass norm kernel holds in registers
+
+struct DevBuf {
+  void* p = nullptr;
+  cudaError_t alloc(size_t bytes) { return cudaMalloc(&p, bytes ? bytes : 1); }
+  ~DevBuf() {
+    if (p) cudaFree(p);
+  }
+};
+
+int device_sms(int* dev) {
+  int sms = 0;
+  if (cudaGetDevice(dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, *dev) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  return sms;
+}
+
+// True when p is memory the current device's kernels can read in place (its own, or managed); anything else is copied first.
+bool on_device(const void* p) {
+  cudaPointerAttributes at;
+  int cur = -1;
+  if (cudaGetDevice(&cur) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  return (at.type == cudaMemoryTypeDevice && at.device == cur) || at.type == cudaMemoryTypeManaged;
+}
+
+// Canonical codes [N, K] -> device layout: one thread per 16-byte piece of the result.
+__global__ void import_kernel(const uint8_t* __restrict__ src, int N, int K, int Np, int Kb, uint8_t* __restrict__ dst) {
+  const size_t total = (size_t)Kb * Np * 8;
+  const bool wide = K % 16 == 0 && (reinterpret_cast<uintptr_t>(src) & 15) == 0;
+  for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < total; i += (size_t)gridDim.x * blockDim.x) {
+    const int piece = (int)(i & 7), n = (int)((i >> 3) % Np), kb = (int)((i >> 3) / Np);
+    const int k = kb * 128 + ((piece ^ (n & 7)) << 4);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (n < N && k < K) {
+      const uint8_t* s = src + (size_t)n * K + k;
+      if (wide) {
+        v = *reinterpret_cast<const uint4*>(s);
+      } else {
+        uint8_t* b = reinterpret_cast<uint8_t*>(&v);
+        for (int j = 0; j < 16; ++j)
+          if (k + j < K) b[j] = s[j];
+      }
+    }
+    reinterpret_cast<uint4*>(dst)[i] = v;
+  }
+}
+
+__global__ void import_scales_kernel(const uint8_t* __restrict__ src, int Nb, int Kb, int P, uint8_t* __restrict__ dst) {
+  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < Nb * P; i += gridDim.x * blockDim.x) {
+    const int nb = i / P, kb = i - nb * P;
+    dst[i] = kb < Kb ? src[(size_t)nb * Kb + kb] : (uint8_t)127;
+  }
+}
+
+__global__ void export_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int N, int K, int Np, int Kb, int P,
+                              uint8_t* __restrict__ out_codes, uint8_t* __restrict__ out_scales) {
+  const size_t total = (size_t)N * K;
+  for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < total; i += (size_t)gridDim.x * blockDim.x) {
+    const int n = (int)(i / K), k = (int)(i - (size_t)n * K);
+    out_codes[i] = codes[xq_f8_code_offset(n, k, Np)];
+    if (n % 128 == 0 && k % 128 == 0) out_scales[(size_t)(n / 128) * Kb + k / 128] = scales[(size_t)(n / 128) * P + k / 128];
+  }
+}
+
+// bf16 weights [N, K] -> codes and scales, one CTA of 256 threads per 128 x 128 block.
+__global__ void __launch_bounds__(256) prepare_kernel(const uint16_t* __restrict__ W, int N, int K, int Np, int P, uint8_t* __restrict__ codes,
+                                                      uint8_t* __restrict__ scales) {
+  __shared__ float red[8];
+  const int kb = blockIdx.x, nb = blockIdx.y, t = threadIdx.x;
+  float v[64], amax = 0.f;  // thread: channel t / 2, codes 64 (t mod 2) .. + 63
+  const int n = nb * 128 + (t >> 1), k0 = kb * 128 + 64 * (t & 1);
+#pragma unroll
+  for (int j = 0; j < 64; ++j) {
+    v[j] = n < N && k0 + j < K ? __uint_as_float((uint32_t)W[(size_t)n * K + k0 + j] << 16) : 0.f;
+    amax = fmaxf(amax, fabsf(v[j]));
+  }
+  for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+  if ((t & 31) == 0) red[t >> 5] = amax;
+  __syncthreads();
+  for (int i = 0; i < 8; ++i) amax = fmaxf(amax, red[i]);
+  const int b = xqf8::scale_byte(amax);
+  const float s = xqf8::inv_scale(b);
+#pragma unroll
+  for (int j = 0; j < 64; j += 4)
+    *reinterpret_cast<uint32_t*>(codes + xq_f8_code_offset(n, k0 + j, Np)) = xqf8::pack4(v[j] * s, v[j + 1] * s, v[j + 2] * s, v[j + 3] * s);
+  if (t == 0) scales[(size_t)nb * P + kb] = (uint8_t)b;
+}
+
+xq_status make_weights(int32_t N, int32_t K, xq_f8_weights** out) {
+  if (N < 1 || K < 1 || N > (1 << 24) || K > (1 << 24)) return XQ_ERR_INVALID_ARG;
+  xq_f8_weights* w = new (std::nothrow) xq_f8_weights();
+  if (!w) return XQ_ERR_ALLOC;
+  w->N = N;
+  w->K = K;
+  w->Np = xq_f8_padded(N);
+  w->Kb = xq_f8_blocks(K);
+  w->codes = nullptr;
+  w->scales = nullptr;
+  w->sms = device_sms(&w->device);
+  if (w->sms == 0) {
+    delete w;
+    return XQ_ERR_CUDA;
+  }
+  if (cudaMalloc((void**)&w->codes, (size_t)w->Kb * w->Np * 128) != cudaSuccess ||
+      cudaMalloc((void**)&w->scales, (size_t)(w->Np / 128) * xq_f8_pitch(K)) != cudaSuccess) {
+    cudaGetLastError();
+    xq_f8_weights_free(w);
+    return XQ_ERR_ALLOC;
+  }
+  *out = w;
+  return XQ_OK;
+}
+
+// Synchronizes; frees the object when something failed.
+xq_status finish_weights(cudaError_t e, xq_f8_weights* w, cudaStream_t st, xq_f8_weights** out) {
+  const cudaError_t s = cudaStreamSynchronize(st);  // also after a failure: nothing may still use the staging buffers
+  if (e == cudaSuccess) e = s;
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    xq_f8_weights_free(w);
+    return XQ_ERR_CUDA;
+  }
+  *out = w;
+  return XQ_OK;
+}
+
+// Workspace: header (status word) | token codes | token scales (what xq_f8_linear keeps between its two kernels).
+struct F8Ws {
+  size_t codes, scales, total;
+};
+F8Ws f8_ws(int32_t M, const xq_f8_weights* w) {
+  F8Ws L;
+  size_t off = XQ_WS_HEADER_BYTES;
+  L.codes = off;
+  off += align_up((size_t)M * w->Kb * 128, 256);
+  L.scales = off;
+  off += align_up((size_t)M * xq_f8_pitch(w->K), 256);
+  L.total = off;
+  return L;
+}
+
+xq_status ws_check(const void* ws, size_t bytes, size_t need) {
+  return !ws || !aligned(ws, 16) || bytes < need ? XQ_ERR_WORKSPACE : XQ_OK;
+}
+
+xq_status status_of(cudaError_t e) {
+  if (e == cudaSuccess) return XQ_OK;
+  cudaGetLastError();
+  return XQ_ERR_CUDA;
+}
+
+bool bad_rows(const void* p, int64_t ld, int32_t K) { return !p || !aligned(p, 16) || ld < K || ld % 8 != 0; }
+
+}  // namespace
+
+extern "C" {
+
+void xq_f8_weights_free(xq_f8_weights* w) {
+  if (!w) return;
+  if (w->codes) cudaFree(w->codes);
+  if (w->scales) cudaFree(w->scales);
+  delete w;
+}
+
+xq_status xq_f8_weights_info(const xq_f8_weights* w, int32_t* N, int32_t* K) {
+  if (!w) return XQ_ERR_INVALID_ARG;
+  if (N) *N = w->N;
+  if (K) *K = w->K;
+  return XQ_OK;
+}
+
+xq_status xq_f8_prepare_weights(const void* W, int32_t N, int32_t K, void* stream, xq_f8_weights** out) {
+  XQ_RANGE();
+  if (!W || !out) return XQ_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  xq_f8_weights* w = nullptr;
+  xq_status s = make_weights(N, K, &w);
+  if (s != XQ_OK) return s;
+  DevBuf dW;
+  const void* src = W;
+  cudaError_t e = cudaSuccess;
+  if (!on_device(W)) {
+    if (dW.alloc((size_t)N * K * 2) != cudaSuccess) {
+      cudaGetLastError();
+      xq_f8_weights_free(w);
+      return XQ_ERR_ALLOC;
+    }
+    e = cudaMemcpyAsync(dW.p, W, (size_t)N * K * 2, cudaMemcpyDefault, st);
+    src = dW.p;
+  }
+  const int P = xq_f8_pitch(K);
+  if (e == cudaSuccess) e = cudaMemsetAsync(w->scales, 127, (size_t)(w->Np / 128) * P, st);
+  // the grid's second dimension is limited to 65535 blocks: N up to 2^24 has at most 131072 block rows
+  for (int nb = 0; nb < w->Np / 128 && e == cudaSuccess; nb += 65535) {
+    const int rows = w->Np / 128 - nb < 65535 ? w->Np / 128 - nb : 65535;
+    prepare_kernel<<<dim3(w->Kb, rows), 256, 0, st>>>((const uint16_t*)src + (size_t)nb * 128 * K, N - nb * 128, K, w->Np, P,
+                                                      w->codes + (size_t)nb * 128 * 128, w->scales + (size_t)nb * P);
+    e = cudaGetLastError();
+  }
+  return finish_weights(e, w, st, out);
+}
+
+xq_status xq_f8_weights_import(const uint8_t* codes, const uint8_t* scales, int32_t N, int32_t K, void* stream, xq_f8_weights** out) {
+  XQ_RANGE();
+  if (!codes || !scales || !out) return XQ_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  xq_f8_weights* w = nullptr;
+  xq_status s = make_weights(N, K, &w);
+  if (s != XQ_OK) return s;
+  const int Nb = w->Np / 128;
+  const size_t nc = (size_t)N * K, ns = (size_t)Nb * w->Kb;
+  std::vector<uint8_t> host;
+  try {
+    host.resize(ns);
+  } catch (const std::bad_alloc&) {
+    xq_f8_weights_free(w);
+    return XQ_ERR_ALLOC;
+  }
+  // the scales are looked at on the host, wherever they are: 255 is NaN
+  cudaError_t e = cudaMemcpyAsync(host.data(), scales, ns, cudaMemcpyDefault, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    xq_f8_weights_free(w);
+    return XQ_ERR_CUDA;
+  }
+  if (memchr(host.data(), 255, ns)) {
+    xq_f8_weights_free(w);
+    return XQ_ERR_INVALID_ARG;
+  }
+  DevBuf dC, dS;
+  const bool in_place = on_device(codes);
+  if ((!in_place && dC.alloc(nc) != cudaSuccess) || dS.alloc(ns) != cudaSuccess) {
+    cudaGetLastError();
+    xq_f8_weights_free(w);
+    return XQ_ERR_ALLOC;
+  }
+  e = cudaMemcpyAsync(dS.p, host.data(), ns, cudaMemcpyHostToDevice, st);
+  if (e == cudaSuccess && !in_place) e = cudaMemcpyAsync(dC.p, codes, nc, cudaMemcpyDefault, st);
+  if (e == cudaSuccess) {
+    import_kernel<<<w->sms * 8, 256, 0, st>>>(in_place ? codes : (const uint8_t*)dC.p, N, K, w->Np, w->Kb, w->codes);
+    e = cudaGetLastError();
+  }
+  if (e == cudaSuccess) {
+    import_scales_kernel<<<w->sms, 256, 0, st>>>((const uint8_t*)dS.p, Nb, w->Kb, xq_f8_pitch(K), w->scales);
+    e = cudaGetLastError();
+  }
+  return finish_weights(e, w, st, out);
+}
+
+xq_status xq_f8_weights_export(const xq_f8_weights* w, uint8_t* codes, uint8_t* scales) {
+  XQ_RANGE();
+  if (!w || !codes || !scales || !xq_on_device(w->device)) return XQ_ERR_INVALID_ARG;
+  const size_t nc = (size_t)w->N * w->K, ns = (size_t)(w->Np / 128) * w->Kb;
+  DevBuf dC, dS;
+  if (dC.alloc(nc) != cudaSuccess || dS.alloc(ns) != cudaSuccess) {
+    cudaGetLastError();
+    return XQ_ERR_ALLOC;
+  }
+  export_kernel<<<w->sms * 8, 256>>>(w->codes, w->scales, w->N, w->K, w->Np, w->Kb, xq_f8_pitch(w->K), (uint8_t*)dC.p, (uint8_t*)dS.p);
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess) e = cudaMemcpy(codes, dC.p, nc, cudaMemcpyDeviceToHost);
+  if (e == cudaSuccess) e = cudaMemcpy(scales, dS.p, ns, cudaMemcpyDeviceToHost);
+  return status_of(e);
+}
+
+size_t xq_f8_workspace_bytes(int32_t M_max, const xq_f8_weights* w) {
+  if (!w || M_max < 1) return 0;
+  return f8_ws(M_max, w).total;
+}
+
+xq_status xq_f8_quant(const void* X, int32_t M, int32_t K, int64_t ldx, uint8_t* codes, uint8_t* scales, void* stream) {
+  XQ_RANGE();
+  if (M < 0 || K < 1 || K > kMaxRow) return XQ_ERR_INVALID_ARG;
+  if (M == 0) return XQ_OK;
+  if (bad_rows(X, ldx, K) || !codes || !scales || !aligned(codes, 16) || !aligned(scales, 4)) return XQ_ERR_INVALID_ARG;
+  int dev = 0;
+  const int sms = device_sms(&dev);
+  if (sms == 0) return XQ_ERR_CUDA;
+  const XqF8NormArgs a = {X, ldx, nullptr, 0, nullptr, 0.f, M, K, nullptr, nullptr, 0, codes, scales};
+  return status_of(xq_f8_launch_norm_quant(a, sms, (cudaStream_t)stream));
+}
+
+xq_status xq_f8_norm_quant(const void* X, int32_t M, int32_t K, int64_t ldx, const void* residual_opt, int64_t ldr, const void* gamma,
+                           float eps, void* sum_opt, uint8_t* codes, uint8_t* scales, void* Y_opt, int64_t ldy, void* stream) {
+  XQ_RANGE();
+  if (M < 0 || K < 1 || K > kMaxRow || !(eps >= 0.f)) return XQ_ERR_INVALID_ARG;
+  if (M == 0) return XQ_OK;
+  if (bad_rows(X, ldx, K) || !gamma || !aligned(gamma, 16) || !codes || !scales || !aligned(codes, 16) || !aligned(scales, 4))
+    return XQ_ERR_INVALID_ARG;
+  if ((residual_opt && bad_rows(residual_opt, ldr, K)) || (sum_opt && bad_rows(sum_opt, ldr, K)) || (Y_opt && bad_rows(Y_opt, ldy, K)))
+    return XQ_ERR_INVALID_ARG;
+  int dev = 0;
+  const int sms = device_sms(&dev);
+  if (sms == 0) return XQ_ERR_CUDA;
+  const XqF8NormArgs a = {X, ldx, residual_opt, ldr, gamma, eps, M, K, sum_opt, Y_opt, ldy, codes, scales};
+  return status_of(xq_f8_launch_norm_quant(a, sms, (cudaStream_t)stream));
+}
+
+xq_status xq_f8_gemm(const uint8_t* codes, const uint8_t* scales, int32_t M, const xq_f8_weights* w, void* out, void* ws, size_t ws_bytes,
+                     void* stream) {
+  XQ_RANGE();
+  if (!w || M < 0) return XQ_ERR_INVALID_ARG;
+  if (M == 0) return XQ_OK;
+  if (!codes || !scales || !out || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(out, 16) || !xq_on_device(w->device))
+    return XQ_ERR_INVALID_ARG;
+  const xq_status s = ws_check(ws, ws_bytes, XQ_WS_HEADER_BYTES);
+  if (s != XQ_OK) return s;
+  return status_of(xq_f8_launch_gemm(codes, scales, M, w, out, (int32_t*)ws, (cudaStream_t)stream));
+}
+
+xq_status xq_f8_linear(const void* X, int32_t M, int64_t ldx, const xq_f8_weights* w, void* out, void* ws, size_t ws_bytes, void* stream) {
+  XQ_RANGE();
+  if (!w || M < 0) return XQ_ERR_INVALID_ARG;
+  if (M == 0) return XQ_OK;
+  if (bad_rows(X, ldx, w->K) || w->K > kMaxRow || !out || !aligned(out, 16) || !xq_on_device(w->device)) return XQ_ERR_INVALID_ARG;
+  const F8Ws L = f8_ws(M, w);
+  const xq_status s = ws_check(ws, ws_bytes, L.total);
+  if (s != XQ_OK) return s;
+  uint8_t* base = (uint8_t*)ws;
+  cudaStream_t st = (cudaStream_t)stream;
+  const XqF8NormArgs a = {X, ldx, nullptr, 0, nullptr, 0.f, M, w->K, nullptr, nullptr, 0, base + L.codes, base + L.scales};
+  cudaError_t e = xq_f8_launch_norm_quant(a, w->sms, st);
+  if (e == cudaSuccess) e = xq_f8_launch_gemm(base + L.codes, base + L.scales, M, w, out, (int32_t*)ws, st);
+  return status_of(e);
+}
+
+xq_status xq_f8_gated(const uint8_t* codes, const uint8_t* scales, int32_t M, const xq_f8_weights* gate, const xq_f8_weights* up,
+                      void* out_bf16_opt, uint8_t* out_codes_opt, uint8_t* out_scales_opt, void* ws, size_t ws_bytes, void* stream) {
+  XQ_RANGE();
+  if (!gate || !up || M < 0 || gate->N != up->N || gate->K != up->K) return XQ_ERR_INVALID_ARG;
+  // one result: bf16 rows, or 8-bit rows (both of their arrays)
+  if ((out_bf16_opt != nullptr) == (out_codes_opt != nullptr) || (out_codes_opt != nullptr) != (out_scales_opt != nullptr)) {
+    if (M > 0) return XQ_ERR_INVALID_ARG;
+  }
+  if (M == 0) return XQ_OK;
+  if (!codes || !scales || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(out_bf16_opt, 16) || !aligned(out_codes_opt, 16) ||
+      !aligned(out_scales_opt, 4) || !xq_on_device(gate->device) || up->device != gate->device)
+    return XQ_ERR_INVALID_ARG;
+  const xq_status s = ws_check(ws, ws_bytes, XQ_WS_HEADER_BYTES);
+  if (s != XQ_OK) return s;
+  return status_of(xq_f8_launch_gated(codes, scales, M, gate, up, out_bf16_opt, out_codes_opt, out_scales_opt, (int32_t*)ws,
+                                      (cudaStream_t)stream));
+}
+
+}  // extern "C"

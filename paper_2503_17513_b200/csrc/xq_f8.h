@@ -1,0 +1,93 @@
+// Internal declarations of the 8-bit floating-point layer (xq_f8_*): the number format, the weights object, the launchers.
+//
+// Format: E4M3 elements, one E8M0 scale byte b (the power of two 2^(b - 127)) per group of 128 consecutive channels of a
+// token row and per 128 x 128 block of a weight matrix.
+//
+// Weights in device memory (library-owned):
+//   codes  [Kb][Np][128 bytes], Kb = ceil(K / 128), Np = N rounded up to 128: the 128 codes of one output channel at one K block
+//          are 128 contiguous bytes, their eight 16-byte pieces stored at piece index XOR (channel mod 8).  That is the 128-byte
+//          shared-memory swizzle of the tensor core, so any run of channels whose start is a multiple of eight is ONE contiguous
+//          copy that lands as a ready operand tile, and a 128-channel tile at one K block is 16 KiB of consecutive addresses.
+//   scales [Np / 128][P bytes], P = Kb rounded up to four: the scale bytes of four consecutive K blocks are one 32-bit word,
+//          which is the word the block-scaled MMA reads from tensor memory (byte j of the word for the K block 4 i + j).
+// Padding: zero codes, scale byte 127 (a scale of one; never 255, which is NaN).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "xq.h"
+
+constexpr int XQ_F8_GROUP = 128;
+
+struct xq_f8_weights {
+  int32_t N, K;     // logical sizes
+  int32_t Np, Kb;   // N rounded up to 128, number of K blocks
+  uint8_t* codes;   // device, Kb * Np * 128
+  uint8_t* scales;  // device, (Np / 128) * P
+  int device, sms;
+};
+
+__host__ __device__ inline int xq_f8_blocks(int K) { return (K + XQ_F8_GROUP - 1) / XQ_F8_GROUP; }
+__host__ __device__ inline int xq_f8_padded(int K) { return xq_f8_blocks(K) * XQ_F8_GROUP; }
+// bytes of scales per token row: one per group, rounded up so that four groups are one aligned word
+__host__ __device__ inline int xq_f8_pitch(int K) { return (xq_f8_blocks(K) + 3) / 4 * 4; }
+// byte offset of code k of channel n in the weights object
+__host__ __device__ inline size_t xq_f8_code_offset(int n, int k, int Np) {
+  return ((size_t)(k >> 7) * Np + n) * 128 + (size_t)((((k >> 4) & 7) ^ (n & 7)) << 4) + (k & 15);
+}
+
+#ifdef __CUDACC__
+namespace xqf8 {
+
+// Scale byte of a group: the smallest e with amax <= 448 * 2^e, plus 127; 127 for a group of zeros.  448 = 1.75 * 2^8, so e is
+// the exponent of amax less 8, one more when the mantissa is above 1.75: the carry of the addition.  An infinite amax gives
+// 247, and 448 * 2^120 is beyond the fp32 range: the infinity survives.  Below 2^-119 the byte stays at 0.
+__device__ __forceinline__ int scale_byte(float amax) {
+  if (amax == 0.f) return 127;
+  const int b = (int)((__float_as_uint(amax) + 0x1FFFFFu) >> 23) - 8;
+  return b < 0 ? 0 : b;
+}
+// 2^(127 - b), exact for every byte scale_byte can return (0..247)
+__device__ __forceinline__ float inv_scale(int b) { return __uint_as_float((uint32_t)(254 - b) << 23); }
+// four values, scaled -> four E4M3 bytes (round to nearest even; NaN stays NaN)
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+  return lo | (hi << 16);
+}
+__device__ __forceinline__ float decode(uint8_t v) {
+  __nv_fp8_e4m3 q;
+  q.__x = v;
+  return (float)q;
+}
+
+}  // namespace xqf8
+#endif
+
+// ---- launchers (each returns the CUDA error of its launch) -----------------------------------------------------------
+struct XqF8NormArgs {
+  const void* x;         // bf16 [M, ldx]
+  int64_t ldx;
+  const void* residual;  // bf16 [M, ldr] or null
+  int64_t ldr;
+  const void* gamma;     // bf16 [K]; null: no norm, the rows are quantized as they are
+  float eps;
+  int32_t M, K;
+  void* sum;             // bf16 [M, ldr] or null; may be the residual
+  void* y;               // bf16 [M, ldy] or null
+  int64_t ldy;
+  uint8_t* codes;        // [M, Kq]
+  uint8_t* scales;       // [M, P]
+};
+cudaError_t xq_f8_launch_norm_quant(const XqF8NormArgs& a, int sms, cudaStream_t st);
+
+// out bf16 [M, N] = tokens x w^T.
+cudaError_t xq_f8_launch_gemm(const uint8_t* codes, const uint8_t* scales, int32_t M, const xq_f8_weights* w, void* out,
+                              int32_t* status, cudaStream_t st);
+// silu(tokens x gate^T) * (tokens x up^T), either bf16 [M, N] (out) or 8-bit rows (out_codes, out_scales).
+cudaError_t xq_f8_launch_gated(const uint8_t* codes, const uint8_t* scales, int32_t M, const xq_f8_weights* gate,
+                               const xq_f8_weights* up, void* out, uint8_t* out_codes, uint8_t* out_scales, int32_t* status,
+                               cudaStream_t st);

@@ -44,6 +44,8 @@ EXPORTS = [
     "xq_mx_workspace_bytes", "xq_mx_rotate_quant", "xq_mx_gemm", "xq_mx_expanded_linear",
     "xq_mx_expanded_linear_host", "xq_mx_gemm_staged", "xq_mx_rotate_quant_staged",
     "xq_mx_prepare_weights_heads", "xq_mx_weights_heads", "xq_gemm_kernel_info", "xq_selftest_i8_mma_rate", "xq_expanded_linear_host_enqueue", "xq_expanded_linear_one_launch", "xq_prepare_weights_gptq", "xq_gptq_codes",
+    "xq_f8_prepare_weights", "xq_f8_weights_import", "xq_f8_weights_export", "xq_f8_weights_info", "xq_f8_weights_free", "xq_f8_quant",
+    "xq_f8_norm_quant", "xq_f8_workspace_bytes", "xq_f8_gemm", "xq_f8_linear", "xq_f8_gated",
 ]
 
 
@@ -108,9 +110,22 @@ def lib() -> ctypes.CDLL:
         L.xq_selftest_wait_timeout.argtypes = [vp, sz, vp]
         L.xq_selftest_i8_mma_rate.argtypes = [i32, vp, sz, vp, ctypes.POINTER(ctypes.c_double)]
         L.xq_gemm_kernel_info.argtypes = [i32, vp, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i32)]
+        L.xq_f8_prepare_weights.argtypes = [vp, i32, i32, vp, ctypes.POINTER(vp)]
+        L.xq_f8_weights_import.argtypes = [vp, vp, i32, i32, vp, ctypes.POINTER(vp)]
+        L.xq_f8_weights_export.argtypes = [vp, vp, vp]
+        L.xq_f8_weights_info.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i32)]
+        L.xq_f8_weights_free.argtypes = [vp]
+        L.xq_f8_weights_free.restype = None
+        L.xq_f8_quant.argtypes = [vp, i32, i32, i64, vp, vp, vp]
+        L.xq_f8_norm_quant.argtypes = [vp, i32, i32, i64, vp, i64, vp, ctypes.c_float, vp, vp, vp, vp, i64, vp]
+        L.xq_f8_workspace_bytes.argtypes = [i32, vp]
+        L.xq_f8_workspace_bytes.restype = sz
+        L.xq_f8_gemm.argtypes = [vp, vp, i32, vp, vp, vp, sz, vp]
+        L.xq_f8_linear.argtypes = [vp, i32, i64, vp, vp, vp, sz, vp]
+        L.xq_f8_gated.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
         for name in EXPORTS:
             if name not in ("xq_status_string", "xq_weights_free", "xq_workspace_bytes", "xq_weights_heads", "xq_mx_weights_free",
-                            "xq_mx_workspace_bytes", "xq_mx_weights_heads"):
+                            "xq_mx_workspace_bytes", "xq_mx_weights_heads", "xq_f8_weights_free", "xq_f8_workspace_bytes"):
                 getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -454,3 +469,131 @@ def xq_mx_prepare_weights_heads(W_bf16_host: np.ndarray, heads: int, head_dim_p:
     _check(lib().xq_mx_prepare_weights_heads(_hp(W), N, heads, K // heads, head_dim_p, _stream(stream), ctypes.byref(h)),
            "xq_mx_prepare_weights_heads")
     return MxWeights(h.value)
+
+
+# ---- 8-bit floating-point layer --------------------------------------------------------------------
+
+class F8Weights:
+    """Owner of one ``xq_f8_weights*`` (freed with the object)."""
+
+    def __init__(self, handle: int):
+        self.handle = ctypes.c_void_p(handle)
+        n, k = ctypes.c_int32(), ctypes.c_int32()
+        _check(lib().xq_f8_weights_info(self.handle, ctypes.byref(n), ctypes.byref(k)), "xq_f8_weights_info")
+        self.N, self.K = n.value, k.value
+
+    def free(self):
+        if self.handle:
+            lib().xq_f8_weights_free(self.handle)
+            self.handle = ctypes.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def f8_padded(K: int) -> int:
+    """Bytes of a token row's codes: K rounded up to whole groups of 128."""
+    return -(-K // 128) * 128
+
+
+def f8_scale_pitch(K: int) -> int:
+    """Bytes of a token row's scales: one per group of 128, rounded up to four."""
+    return -(-K // 512) * 4
+
+
+def new_f8_rows(M: int, K: int, device="cuda"):
+    """Allocate (with torch) 8-bit token rows: (codes [M, f8_padded(K)], scales [M, f8_scale_pitch(K)])."""
+    return (torch.empty((M, f8_padded(K)), dtype=torch.uint8, device=device),
+            torch.empty((M, f8_scale_pitch(K)), dtype=torch.uint8, device=device))
+
+
+def _any(a, dtype: np.dtype, shape):
+    """(owner, address) of a contiguous host array or torch tensor of `shape` whose elements have the size of `dtype`."""
+    if isinstance(a, torch.Tensor):
+        a = a.contiguous()
+        assert a.element_size() == dtype.itemsize and (shape is None or tuple(a.shape) == tuple(shape))
+        return a, ctypes.c_void_p(a.data_ptr())
+    a = np.ascontiguousarray(a)
+    assert a.dtype.itemsize == dtype.itemsize and (shape is None or a.shape == tuple(shape))
+    return a, _hp(a)
+
+
+def xq_f8_prepare_weights(W_bf16, stream=None) -> F8Weights:
+    """W: bf16 [N, K] (out x in): a host array of 16-bit patterns or a torch tensor, on the host or the device."""
+    N, K = W_bf16.shape
+    W, p = _any(W_bf16, np.dtype(np.uint16), None)
+    h = ctypes.c_void_p()
+    _check(lib().xq_f8_prepare_weights(p, N, K, _stream(stream), ctypes.byref(h)), "xq_f8_prepare_weights")
+    return F8Weights(h.value)
+
+
+def xq_f8_weights_import(codes, scales, stream=None) -> F8Weights:
+    """codes [N, K] E4M3 bytes, scales [ceil(N / 128), ceil(K / 128)] E8M0 bytes: host arrays or torch tensors."""
+    N, K = codes.shape
+    c, cp = _any(codes, np.dtype(np.uint8), None)
+    s, sp = _any(scales, np.dtype(np.uint8), (-(-N // 128), -(-K // 128)))
+    h = ctypes.c_void_p()
+    _check(lib().xq_f8_weights_import(cp, sp, N, K, _stream(stream), ctypes.byref(h)), "xq_f8_weights_import")
+    return F8Weights(h.value)
+
+
+def xq_f8_weights_export(w: F8Weights):
+    codes = np.empty((w.N, w.K), dtype=np.uint8)
+    scales = np.empty((-(-w.N // 128), -(-w.K // 128)), dtype=np.uint8)
+    _check(lib().xq_f8_weights_export(w.handle, _hp(codes), _hp(scales)), "xq_f8_weights_export")
+    return codes, scales
+
+
+def new_f8_workspace(M_max: int, w: F8Weights, device="cuda") -> torch.Tensor:
+    ws = torch.empty(int(lib().xq_f8_workspace_bytes(M_max, w.handle)), dtype=torch.uint8, device=device)
+    xq_workspace_init(ws)
+    return ws
+
+
+def _rows(t):
+    """(address, row pitch) of a 2-D device tensor whose rows are contiguous; (null, 0) for None."""
+    if t is None:
+        return ctypes.c_void_p(0), 0
+    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)
+    return ctypes.c_void_p(t.data_ptr()), t.stride(0)
+
+
+def xq_f8_quant(X, codes, scales, stream=None) -> None:
+    p, ldx = _rows(X)
+    _check(lib().xq_f8_quant(p, X.shape[0], X.shape[1], ldx, _dp(codes), _dp(scales), _stream(stream)), "xq_f8_quant")
+
+
+def xq_f8_norm_quant(X, gamma, eps: float, codes, scales, residual=None, sum_out=None, y=None, stream=None) -> None:
+    """residual and sum_out may be the same tensor; if both are given their row pitches must be equal."""
+    p, ldx = _rows(X)
+    rp, ldr = _rows(residual)
+    sp, lds = _rows(sum_out)
+    yp, ldy = _rows(y)
+    M, K = X.shape
+    assert residual is None or sum_out is None or ldr == lds
+    for t in (residual, sum_out, y):
+        assert t is None or t.shape == X.shape
+    assert gamma.numel() == K
+    _check(lib().xq_f8_norm_quant(p, M, K, ldx, rp, ldr or lds, _dp(gamma), eps, sp, _dp(codes), _dp(scales), yp, ldy, _stream(stream)),
+           "xq_f8_norm_quant")
+
+
+def xq_f8_gemm(codes, scales, M: int, w: F8Weights, out, ws, stream=None) -> None:
+    _check(lib().xq_f8_gemm(_dp(codes), _dp(scales), M, w.handle, _dp(out), _dp(ws), ws.numel() * ws.element_size(), _stream(stream)),
+           "xq_f8_gemm")
+
+
+def xq_f8_linear(X, w: F8Weights, out, ws, M=None, ldx=None, stream=None) -> None:
+    M = X.shape[0] if M is None else M
+    ldx = X.stride(0) if ldx is None else ldx
+    _check(lib().xq_f8_linear(ctypes.c_void_p(X.data_ptr()), M, ldx, w.handle, _dp(out), _dp(ws), ws.numel() * ws.element_size(),
+                              _stream(stream)), "xq_f8_linear")
+
+
+def xq_f8_gated(codes, scales, M: int, gate: F8Weights, up: F8Weights, ws, out=None, out_codes=None, out_scales=None, stream=None) -> None:
+    """silu(tokens x gate^T) * (tokens x up^T): bf16 rows into `out`, or 8-bit rows into `out_codes` and `out_scales`."""
+    _check(lib().xq_f8_gated(_dp(codes), _dp(scales), M, gate.handle, up.handle, _dp(out), _dp(out_codes), _dp(out_scales), _dp(ws),
+                             ws.numel() * ws.element_size(), _stream(stream)), "xq_f8_gated")
