@@ -329,7 +329,8 @@ xq_status xq_f8_gemm(const uint8_t* codes, const uint8_t* scales, int32_t M, con
     return XQ_ERR_INVALID_ARG;
   const xq_status s = ws_check(ws, ws_bytes, XQ_WS_HEADER_BYTES);
   if (s != XQ_OK) return s;
-  return status_of(xq_f8_launch_gemm(codes, scales, M, w, out, (int32_t*)ws, (cudaStream_t)stream));
+  const XqF8GemmArgs a = {codes, scales, M, {w, nullptr}, out, nullptr, nullptr, (int32_t*)ws};
+  return status_of(xq_f8_launch_gemm(a, (cudaStream_t)stream));
 }
 
 xq_status xq_f8_linear(const void* X, int32_t M, int64_t ldx, const xq_f8_weights* w, void* out, void* ws, size_t ws_bytes, void* stream) {
@@ -344,7 +345,8 @@ xq_status xq_f8_linear(const void* X, int32_t M, int64_t ldx, const xq_f8_weight
   cudaStream_t st = (cudaStream_t)stream;
   const XqF8NormArgs a = {X, ldx, nullptr, 0, nullptr, 0.f, M, w->K, nullptr, nullptr, 0, base + L.codes, base + L.scales};
   cudaError_t e = xq_f8_launch_norm_quant(a, w->sms, st);
-  if (e == cudaSuccess) e = xq_f8_launch_gemm(base + L.codes, base + L.scales, M, w, out, (int32_t*)ws, st);
+  const XqF8GemmArgs g = {base + L.codes, base + L.scales, M, {w, nullptr}, out, nullptr, nullptr, (int32_t*)ws};
+  if (e == cudaSuccess) e = xq_f8_launch_gemm(g, st);
   return status_of(e);
 }
 
@@ -362,8 +364,8 @@ xq_status xq_f8_gated(const uint8_t* codes, const uint8_t* scales, int32_t M, co
     return XQ_ERR_INVALID_ARG;
   const xq_status s = ws_check(ws, ws_bytes, XQ_WS_HEADER_BYTES);
   if (s != XQ_OK) return s;
-  return status_of(xq_f8_launch_gated(codes, scales, M, gate, up, out_bf16_opt, out_codes_opt, out_scales_opt, (int32_t*)ws,
-                                      (cudaStream_t)stream));
+  const XqF8GemmArgs a = {codes, scales, M, {gate, up}, out_bf16_opt, out_codes_opt, out_scales_opt, (int32_t*)ws};
+  return status_of(xq_f8_launch_gemm(a, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -58,11 +58,7 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
   const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
   return lo | (hi << 16);
 }
-__device__ __forceinline__ float decode(uint8_t v) {
-  __nv_fp8_e4m3 q;
-  q.__x = v;
-  return (float)q;
-}
+__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + expf(-g)) * u; }
 
 }  // namespace xqf8
 #endif
@@ -84,10 +80,18 @@ struct XqF8NormArgs {
 };
 cudaError_t xq_f8_launch_norm_quant(const XqF8NormArgs& a, int sms, cudaStream_t st);
 
-// out bf16 [M, N] = tokens x w^T.
-cudaError_t xq_f8_launch_gemm(const uint8_t* codes, const uint8_t* scales, int32_t M, const xq_f8_weights* w, void* out,
-                              int32_t* status, cudaStream_t st);
-// silu(tokens x gate^T) * (tokens x up^T), either bf16 [M, N] (out) or 8-bit rows (out_codes, out_scales).
-cudaError_t xq_f8_launch_gated(const uint8_t* codes, const uint8_t* scales, int32_t M, const xq_f8_weights* gate,
-                               const xq_f8_weights* up, void* out, uint8_t* out_codes, uint8_t* out_scales, int32_t* status,
-                               cudaStream_t st);
+// One product (w[1] null; out) or the gated pair (w[0] gate, w[1] up; out, or out_codes with out_scales).
+struct XqF8GemmArgs {
+  const uint8_t *codes, *scales;  // tokens
+  int32_t M;
+  const xq_f8_weights* w[2];
+  void* out;
+  uint8_t *out_codes, *out_scales;
+  int32_t* status;
+};
+cudaError_t xq_f8_launch_gemm(const XqF8GemmArgs& a, cudaStream_t st);
+// its kernels: weights as the streamed operand (few tokens)
+cudaError_t xq_f8_launch_stream(const XqF8GemmArgs& a, cudaStream_t st);
+
+// Tensor map of 8-bit token rows [rows, pitch bytes]: boxes of 128 bytes x box_rows in the 128-byte swizzle.
+bool xq_f8_map_rows(CUtensorMap* map, const void* p, int rows, int pitch, int box_rows);

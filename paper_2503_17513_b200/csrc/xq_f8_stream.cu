@@ -1,0 +1,324 @@
+// Block-scaled E4M3 products with the weights as the streamed operand (few tokens):
+//   out[m][n] = bf16( sum over K blocks g of 2^(ex[m][g] + ew[n / 128][g]) * sum over k in g of qx[m][k] qw[n][k] )
+// and the gated pair silu(G) * U of two such products over the same tokens.
+//
+// Bound by HBM: the weights cross once (N K bytes), the tokens are small.  128 output channels are the 128 rows of the MMA and
+// the tokens its NT columns, so that no CUDA core touches a weight byte: the 16 KiB of a 128-channel tile at one K block are one
+// bulk copy of consecutive addresses that lands as a ready operand (the weights are stored swizzled), and the tensor core applies
+// the scales of both operands (kind::mxf8f6f4).  K is cut into S slices over a cluster of S CTAs so that every multiprocessor
+// streams; the partial tiles meet in distributed shared memory, added in slice order (the result does not depend on timing).
+#include <cuda_bf16.h>
+
+#include "xq_f8.h"
+#include "xq_f8_mma.cuh"
+#include "xq_internal.h"
+
+using namespace xqptx;
+
+namespace {
+
+struct StreamParams {
+  const uint8_t* w[2];   // weights (gate, up), blocked layout
+  const uint8_t* sw[2];  // their scales
+  const uint8_t* sx;     // token scales [M, P]
+  __nv_bfloat16* out;    // [M, N] or null
+  uint8_t *out_codes, *out_scales;
+  int32_t* status;
+  int M, N, Np, Kb, P, S;
+};
+
+constexpr int kThreads = 7 * 32;
+constexpr int kSfRing = 4;  // scale words of four K blocks each, in shared memory
+
+// NT: token columns of a tile; MATS: 1, or 2 for the gated pair
+template <int NT, int MATS>
+struct StreamCfg {
+  static constexpr int kStageBytes = MATS * 16384 + NT * 128;
+  static constexpr int kSfBytes = (MATS + 1) * 512;
+  // two CTAs on a multiprocessor (113 KiB each) where three stages fit, else one
+  static constexpr int kHalf = 113 * 1024 - 2048 - kSfRing * kSfBytes, kWhole = 226 * 1024 - 2048 - kSfRing * kSfBytes;
+  static constexpr int kPerSm = kHalf / kStageBytes >= 3 ? 2 : 1;
+  static constexpr int kBudget = kPerSm == 2 ? kHalf : kWhole;
+  static constexpr int kStages = kBudget / kStageBytes < 8 ? kBudget / kStageBytes : 8;
+  static constexpr int kRedBytes = MATS * 512 * (NT + 7);  // partial tiles (S * ceil(NT / S) <= NT + 7 columns), in the stages' memory
+  static constexpr int kAccCols = MATS * NT;
+  static constexpr int kSfCol = kAccCols;                // two sets of (MATS + 1) * 4 columns
+  static constexpr int kNeed = kAccCols + 2 * (MATS + 1) * 4;
+  static constexpr int kTmemCols = kNeed <= 64 ? 64 : kNeed <= 128 ? 128 : kNeed <= 256 ? 256 : 512;
+  static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kSfRing * kSfBytes + 256;
+  static_assert(kStages >= 3 && kStages * kStageBytes >= kRedBytes, "stages hold the partial tiles");
+};
+
+template <int NT, int MATS>
+__global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant__ CUtensorMap map_x, const StreamParams p) {
+  using C = StreamCfg<NT, MATS>;
+  constexpr int kStages = C::kStages, kStageBytes = C::kStageBytes;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  unsigned char* base = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  unsigned char* sf = base + (size_t)kStages * kStageBytes;
+  uint64_t* full = reinterpret_cast<uint64_t*>(sf + kSfRing * C::kSfBytes);
+  uint64_t* empty = full + kStages;
+  uint64_t* sf_full = empty + kStages;
+  uint64_t* sf_empty = sf_full + kSfRing;
+  uint64_t* acc_full = sf_empty + kSfRing;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 1);
+  volatile int* failed = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int S = p.S, rank = blockIdx.x % S, tile = blockIdx.x / S, t0 = blockIdx.y * NT;
+  const int mt = p.M - t0 < NT ? p.M - t0 : NT;                                   // tokens of this tile
+  const int kb_lo = rank * p.Kb / S, kb_hi = (rank + 1) * p.Kb / S;               // this CTA's K blocks
+  const int nk = kb_hi - kb_lo;
+  const int g_lo = kb_lo >> 2, g_hi = (kb_hi + 3) >> 2;                           // its scale words
+
+  if (tid == 0) {
+    for (int s = 0; s < kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
+    for (int s = 0; s < kSfRing; ++s) mbar_init(&sf_full[s], 1), mbar_init(&sf_empty[s], 1);
+    mbar_init(acc_full, 1);
+    *failed = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&map_x);
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, C::kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+  pdl_launch_dependents();
+
+  if (warp == 0) {
+    // ---- producer: the weights do not depend on the kernel before this one, the tokens do -------------------------
+    auto load_weights = [&](int i) {
+      unsigned char* st = base + (size_t)(i % kStages) * kStageBytes;
+      mbar_expect_tx(&full[i % kStages], kStageBytes);
+#pragma unroll
+      for (int h = 0; h < MATS; ++h)
+        bulk_g2s(st + h * 16384, p.w[h] + ((size_t)(kb_lo + i) * p.Np + (size_t)tile * 128) * 128, 16384, &full[i % kStages]);
+    };
+    const int pre = nk < kStages ? nk : kStages;
+    if (lane == 0)
+      for (int i = 0; i < pre; ++i) load_weights(i);
+    __syncwarp();
+    pdl_wait();
+    for (int i = 0; i < nk; ++i) {
+      const int s = i % kStages;
+      if (i >= kStages && !mbar_wait_bounded(&empty[s], ((i / kStages) - 1) & 1, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
+      if (lane == 0) {
+        if (i >= kStages) load_weights(i);
+        tma_load_2d(base + (size_t)s * kStageBytes + MATS * 16384, &map_x, (kb_lo + i) * 128, t0, &full[s]);
+      }
+      __syncwarp();
+    }
+  } else if (warp == 1) {
+    // ---- MMA issue ------------------------------------------------------------------------------------------
+    bool ok = true;
+    uint32_t set = 0;
+    for (int i = 0, g = -1; i < nk; ++i) {
+      const int s = i % kStages, kb = kb_lo + i;
+      if (i == 0 || (kb & 3) == 0) {  // the next scale words
+        ++g;
+        ok = mbar_wait_bounded(&sf_full[g % kSfRing], (g / kSfRing) & 1, failed, p.status, (int)XQ_ERR_TIMEOUT);
+        if (!ok) break;
+        tc_fence_after_sync();
+        // two sets of columns in turn: a copy never lands under an instruction that still reads the set before
+        set = tmem + C::kSfCol + (g & 1) * (MATS + 1) * 4;
+        if (lane == 0) {
+          const uint32_t src = smem_u32(sf + (g % kSfRing) * C::kSfBytes);
+#pragma unroll
+          for (int h = 0; h <= MATS; ++h) xqf8::sf_copy<1>(set + 4 * h, xqf8::sf_desc(src + 512 * h));
+          umma_commit(&sf_empty[g % kSfRing]);
+        }
+        __syncwarp();
+      }
+      ok = mbar_wait_bounded(&full[s], (i / kStages) & 1, failed, p.status, (int)XQ_ERR_TIMEOUT);
+      if (!ok) break;
+      tc_fence_after_sync();
+      if (lane == 0) {
+        const uint32_t a = smem_u32(base + (size_t)s * kStageBytes);
+        const uint64_t bdesc = umma_desc_k128(a + MATS * 16384);
+        const uint32_t id = xqf8::idesc(128, NT, kb & 3);
+#pragma unroll
+        for (int h = 0; h < MATS; ++h) {
+          const uint64_t adesc = umma_desc_k128(a + h * 16384);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            xqf8::mma<1>(tmem + h * NT, adesc + 2 * k, bdesc + 2 * k, id, (i | k) != 0 ? 1u : 0u, set + 4 * (1 + h), set);
+        }
+        umma_commit(&empty[s]);
+      }
+      __syncwarp();
+    }
+    // after a failed wait this still signals once everything issued is over, so that nothing is in flight at the end
+    if (lane == 0) umma_commit(acc_full);
+    __syncwarp();
+  } else if (warp == 2) {
+    // ---- scale words: block 0 the tokens', then one block per weight matrix (one word: all 128 channels share it) ----
+    pdl_wait();
+    for (int g = g_lo; g < g_hi; ++g) {
+      const int i = g - g_lo, e = i % kSfRing;
+      if (i >= kSfRing && !mbar_wait_bounded(&sf_empty[e], ((i / kSfRing) - 1) & 1, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
+      uint32_t v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int m = 32 * q + lane;
+        v[q] = m < mt ? *reinterpret_cast<const uint32_t*>(p.sx + (size_t)(t0 + m) * p.P + 4 * g) : 0x7F7F7F7Fu;
+      }
+      uint4* dst = reinterpret_cast<uint4*>(sf + e * C::kSfBytes);
+      dst[lane] = make_uint4(v[0], v[1], v[2], v[3]);
+#pragma unroll
+      for (int h = 0; h < MATS; ++h) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(p.sw[h] + (size_t)tile * p.P + 4 * g);
+        dst[32 * (1 + h) + lane] = make_uint4(w, w, w, w);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sf_full[e]);
+    }
+  }
+
+  // ---- partial tiles to the CTAs that own their tokens: token c belongs to slice c mod S, slot c / S --------------------
+  // [matrix][slice][slot][128 channels] fp32 in the owner's stage memory; every CTA of the cluster must be done with its stages
+  float* red = reinterpret_cast<float*>(base);
+  const int slots = (NT + S - 1) / S;
+  if (warp >= 3) mbar_wait_bounded(acc_full, 0, failed, p.status, (int)XQ_ERR_TIMEOUT);
+  __syncwarp();
+  if (S > 1) {
+    xqf8::cluster_arrive();
+    xqf8::cluster_wait();
+  }
+  if (warp >= 3) {
+    const int q = warp & 3;
+    tc_fence_after_sync();
+    const uint32_t mine = smem_u32(red) + 4 * (q * 32 + lane);
+#pragma unroll 1
+    for (int h = 0; h < MATS; ++h) {
+#pragma unroll 1
+      for (int c0 = 0; c0 < mt; c0 += 16) {
+        uint32_t v[16];
+        tmem_ld_32x16(tmem + ((uint32_t)(q * 32) << 16) + h * NT + c0, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int c = c0 + j;
+          if (c < mt) {
+            const uint32_t at = mine + 512u * (uint32_t)((h * S + rank) * slots + c / S);
+            xqf8::st_cluster(xqf8::map_to(at, c % S), __uint_as_float(v[j]));
+          }
+        }
+      }
+    }
+    tc_fence_before_sync();
+  }
+  if (S > 1) {
+    __syncwarp();
+    xqf8::cluster_arrive();
+    xqf8::cluster_wait();
+  } else {
+    __syncthreads();
+  }
+  // ---- a warp per token: lane = four channels ------------------------------------------------------------------------
+  const int n = tile * 128 + 4 * lane;
+  for (int slot = warp; slot * S + rank < mt; slot += kThreads / 32) {
+    const size_t m = (size_t)t0 + slot * S + rank;
+    float v[MATS][4] = {};
+#pragma unroll
+    for (int h = 0; h < MATS; ++h)
+      for (int s = 0; s < S; ++s) {
+        const float4 t = *reinterpret_cast<const float4*>(red + ((h * S + s) * slots + slot) * 128 + 4 * lane);
+        v[h][0] += t.x, v[h][1] += t.y, v[h][2] += t.z, v[h][3] += t.w;
+      }
+    if (MATS == 2) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[0][j] = xqf8::silu_mul(v[0][j], v[MATS - 1][j]);
+    }
+    if (MATS == 1 || p.out) {
+      __nv_bfloat16* o = p.out + m * p.N + n;
+      if (n + 4 <= p.N && p.N % 4 == 0) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0][0], v[0][1]), hi = __floats2bfloat162_rn(v[0][2], v[0][3]);
+        *reinterpret_cast<uint2*>(o) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (n + j < p.N) o[j] = __float2bfloat16_rn(v[0][j]);
+      }
+    } else {
+      float a = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (n + j >= p.N) v[0][j] = 0.f;
+        a = fmaxf(a, fabsf(v[0][j]));
+      }
+      for (int o = 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+      const int b = xqf8::scale_byte(a);
+      const float sc = xqf8::inv_scale(b);
+      *reinterpret_cast<uint32_t*>(p.out_codes + m * p.Np + n) = xqf8::pack4(v[0][0] * sc, v[0][1] * sc, v[0][2] * sc, v[0][3] * sc);
+      const int Po = xq_f8_pitch(p.N), Gn = p.Np / 128;
+      if (lane == 0) p.out_scales[m * Po + tile] = (uint8_t)b;
+      if (tile == Gn - 1 && lane > 0 && tile + lane < Po) p.out_scales[m * Po + tile + lane] = 127;  // padding of the row's last word
+    }
+  }
+  __syncthreads();
+  if (warp == 0 && *failed)  // bounded drain of copies that may still be landing
+    for (int s = 0; s < kStages; ++s) mbar_wait(&full[s], 0, 1u << 16), mbar_wait(&full[s], 1, 1u << 16);
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, C::kTmemCols);
+  }
+}
+
+template <int NT, int MATS>
+cudaError_t launch(const XqF8GemmArgs& a, cudaStream_t st) {
+  using C = StreamCfg<NT, MATS>;
+  const xq_f8_weights* w = a.w[0];
+  CUtensorMap map_x;
+  if (!xq_f8_map_rows(&map_x, a.codes, a.M, w->Kb * 128, NT)) return cudaErrorInvalidValue;
+  StreamParams p;
+  for (int h = 0; h < 2; ++h) p.w[h] = a.w[h < MATS ? h : 0]->codes, p.sw[h] = a.w[h < MATS ? h : 0]->scales;
+  p.sx = a.scales;
+  p.out = (__nv_bfloat16*)a.out;
+  p.out_codes = a.out_codes;
+  p.out_scales = a.out_scales;
+  p.status = a.status;
+  p.M = a.M;
+  p.N = w->N;
+  p.Np = w->Np;
+  p.Kb = w->Kb;
+  p.P = xq_f8_pitch(w->K);
+  const int tiles = w->Np / 128, rows = (a.M + NT - 1) / NT, slots = w->sms * C::kPerSm;
+  int S = 1;
+  while (S < 8 && (S + 1) * tiles * rows <= slots && (S + 1) * 2 <= w->Kb) ++S;
+  p.S = S;
+  cudaError_t e = cudaFuncSetAttribute(stream_kernel<NT, MATS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemBytes);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(tiles * S, rows);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = C::kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {(unsigned)S, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, stream_kernel<NT, MATS>, map_x, p);
+}
+
+template <int MATS>
+cudaError_t launch_mats(const XqF8GemmArgs& a, cudaStream_t st) {
+  if (a.M <= 16) return launch<16, MATS>(a, st);
+  if (a.M <= 32) return launch<32, MATS>(a, st);
+  if (a.M <= 64 || MATS == 2) return launch<64, MATS>(a, st);
+  return launch<128, MATS>(a, st);
+}
+
+}  // namespace
+
+cudaError_t xq_f8_launch_stream(const XqF8GemmArgs& a, cudaStream_t st) {
+  return a.w[1] ? launch_mats<2>(a, st) : launch_mats<1>(a, st);
+}
