@@ -58,7 +58,9 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
   const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
   return lo | (hi << 16);
 }
-__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + expf(-g)) * u; }
+// silu(g) * u.  The fast exponential and quotient are within 2^-20 relative where the result matters for a sum of magnitude 1
+// (|g| < 8) and within |g| 2^-23 below, far under the 2^-9 of the rounding that follows.
+__device__ __forceinline__ float silu_mul(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
 
 }  // namespace xqf8
 #endif
@@ -92,6 +94,8 @@ struct XqF8GemmArgs {
 cudaError_t xq_f8_launch_gemm(const XqF8GemmArgs& a, cudaStream_t st);
 // its kernels: weights as the streamed operand (few tokens)
 cudaError_t xq_f8_launch_stream(const XqF8GemmArgs& a, cudaStream_t st);
+// 256-token x TN-column tiles on pairs of multiprocessors (many tokens); TN 128, 192 or 256 (the gated pair: 256)
+cudaError_t xq_f8_launch_tile(const XqF8GemmArgs& a, int TN, cudaStream_t st);
 
 // Tensor map of 8-bit token rows [rows, pitch bytes]: boxes of 128 bytes x box_rows in the 128-byte swizzle.
 bool xq_f8_map_rows(CUtensorMap* map, const void* p, int rows, int pitch, int box_rows);

@@ -13,4 +13,7 @@ bool xq_f8_map_rows(CUtensorMap* map, const void* p, int rows, int pitch, int bo
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-cudaError_t xq_f8_launch_gemm(const XqF8GemmArgs& a, cudaStream_t st) { return xq_f8_launch_stream(a, st); }
+// Above 128 tokens the weights are no longer the only traffic that counts: tiles of pairs of multiprocessors.
+cudaError_t xq_f8_launch_gemm(const XqF8GemmArgs& a, cudaStream_t st) {
+  return a.M > 128 ? xq_f8_launch_tile(a, 256, st) : xq_f8_launch_stream(a, st);
+}

@@ -1,0 +1,454 @@
+// Block-scaled E4M3 products for many tokens: 256-token x TN-column tiles on pairs of multiprocessors.
+//   out[m][n] = bf16( sum over K blocks g of 2^(ex[m][g] + ew[n / 128][g]) * sum over k in g of qx[m][k] qw[n][k] )
+// and the gated pair silu(G) * U: a tile then holds the products of 128 channels with both matrices side by side (columns 0-127
+// gate, 128-255 up), so that activation, product and quantization happen on the accumulators.
+//
+// Bound by the tensor cores (2 M N K operations at the E4M3 rate).  One tcgen05.mma of a pair (cta_group::2) multiplies the 256
+// token rows that the two CTAs stage (128 each) with the TN weight rows that they stage (half each): each CTA's shared memory
+// takes in 128 + TN / 2 rows per K block instead of 128 + TN, which is what keeps the operand traffic under the shared-memory
+// bandwidth.  Scales are applied by the instruction, four K blocks per scale word.
+//
+// Roles of a CTA: warp 0 loads (TMA), warp 1 issues MMAs (in the leader, rank 0, for both), warp 2 builds scale words, warps 4-11
+// read the accumulators.  TN = 256 has one accumulator, released as soon as it is in registers; smaller tiles have two.
+#include <cuda_bf16.h>
+
+#include "xq_f8.h"
+#include "xq_f8_mma.cuh"
+#include "xq_internal.h"
+
+using namespace xqptx;
+
+namespace {
+
+struct TileParams {
+  const uint8_t* sw[2];
+  const uint8_t* sx;
+  __nv_bfloat16* out;
+  uint8_t *out_codes, *out_scales;
+  int32_t* status;
+  int M, N, Np, Kb, P, tiles_m, tiles_n;
+};
+
+constexpr int kThreads = 12 * 32;
+constexpr int kEpiWarps = 8;
+
+template <int TN>
+struct TileCfg {
+  static constexpr int kHalfN = TN / 2;
+  static constexpr int kABytes = 128 * 128, kBBytes = kHalfN * 128, kStageBytes = kABytes + kBBytes;
+  static constexpr int kStages = TN == 256 ? 6 : TN == 192 ? 7 : 8;
+  static constexpr int kAccBufs = TN <= 224 ? 2 : 1;
+  static constexpr int kSfbBlocks = (TN + 127) / 128, kSfBytes = 512 * (1 + kSfbBlocks), kSfRing = 3;
+  static constexpr int kSfCols = 4 * (1 + kSfbBlocks);
+  static constexpr int kSfCol = kAccBufs * TN;  // two sets
+  static constexpr int kOutBytes = kEpiWarps * 2048;  // a 32 x 32 bf16 box per epilogue warp
+  static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kOutBytes + kSfRing * kSfBytes + 512;
+  static_assert(kSfCol + 2 * kSfCols <= 512, "tensor memory");
+  static_assert(kSmemBytes <= 232448, "shared memory");
+};
+
+// A wait whose arrivals may come from the other CTA of the pair (cluster scope), bounded like every wait of the library.
+__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, volatile int* failed, int* status) {
+  uint64_t t0 = 0;
+  for (uint32_t i = 1;; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((i & 63u) == 0u) {
+      if (*failed) return false;
+      const uint64_t now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      if (now - t0 > 1000000000ull) break;
+    }
+  }
+  *failed = 1;
+  atomicExch(status, (int)XQ_ERR_TIMEOUT);
+  return false;
+}
+// arrival on a barrier anywhere in the pair (address from map_to)
+__device__ __forceinline__ void arrive_at(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// 2-D tile into this CTA's shared memory, bytes counted on the barrier at `bar` (the leader's)
+__device__ __forceinline__ void load_pair(void* dst, const void* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(
+          smem_u32(dst)),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+// one arrival on the barrier at this offset in both CTAs once everything issued so far is complete
+__device__ __forceinline__ void commit_pair(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+               "h"((uint16_t)3)
+               : "memory");
+}
+
+template <int TN, bool GATED>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w0,
+                const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ CUtensorMap map_o, const TileParams p) {
+  using C = TileCfg<TN>;
+  constexpr int kStages = C::kStages, kStageBytes = C::kStageBytes, kAccBufs = C::kAccBufs, kSfRing = C::kSfRing;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  unsigned char* base = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  unsigned char* outs = base + (size_t)kStages * kStageBytes;
+  unsigned char* sf = outs + C::kOutBytes;
+  uint64_t* full = reinterpret_cast<uint64_t*>(sf + kSfRing * C::kSfBytes);
+  uint64_t* empty = full + kStages;
+  uint64_t* sf_full = empty + kStages;
+  uint64_t* sf_empty = sf_full + kSfRing;
+  uint64_t* acc_full = sf_empty + kSfRing;
+  uint64_t* acc_empty = acc_full + 2;
+  uint64_t* drain = acc_empty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* failed = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = xqf8::cluster_rank();
+  const int tiles = p.tiles_m * p.tiles_n, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+
+  if (tid == 0) {
+    for (int s = 0; s < kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
+    for (int s = 0; s < kSfRing; ++s) mbar_init(&sf_full[s], 2), mbar_init(&sf_empty[s], 1);
+    for (int b = 0; b < 2; ++b) mbar_init(&acc_full[b], 1), mbar_init(&acc_empty[b], 2 * kEpiWarps);
+    mbar_init(drain, 1);
+    *failed = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&map_x);
+    tma_prefetch_desc(rank && GATED ? &map_w1 : &map_w0);
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  // the other CTA's barriers are initialised and its tensor memory allocated before anything is sent there
+  xqf8::cluster_arrive();
+  xqf8::cluster_wait();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 0) {
+    // ---- loads: this CTA's 128 token rows and its half of the weight rows ------------------------------------------
+    pdl_wait();
+    const void* map_w = rank && GATED ? (const void*)&map_w1 : (const void*)&map_w0;
+    bool ok = true;
+    uint32_t it = 0;
+    for (int tile = first; tile < tiles && ok; tile += step) {
+      const int tm = tile % p.tiles_m, tn = tile / p.tiles_m;
+      const int row_x = tm * 256 + (int)rank * 128, row_w = GATED ? tn * 128 : tn * TN + (int)rank * C::kHalfN;
+      for (int kb = 0; kb < p.Kb; ++kb, ++it) {
+        const int s = it % kStages;
+        if (it >= (uint32_t)kStages) {
+          ok = wait_pair(&empty[s], ((it / kStages) - 1) & 1, failed, p.status);
+          if (!ok) break;
+        }
+        if (lane == 0) {
+          unsigned char* st = base + (size_t)s * kStageBytes;
+          const uint32_t bar = xqf8::map_to(smem_u32(&full[s]), 0);
+          if (rank == 0) mbar_expect_tx(&full[s], 2 * kStageBytes);  // both CTAs' copies
+          load_pair(st, &map_x, kb * 128, row_x, bar);
+          load_pair(st + C::kABytes, map_w, 0, kb * p.Np + row_w, bar);
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp == 1) {
+    // ---- MMA issue (the leader, for both) ------------------------------------------------------------------------
+    bool ok = true;
+    uint32_t it = 0, g = 0, tcount = 0;
+    if (rank == 0) {
+      for (int tile = first; tile < tiles && ok; tile += step, ++tcount) {
+        const uint32_t buf = kAccBufs == 2 ? (tcount & 1u) : 0u, use = kAccBufs == 2 ? tcount >> 1 : tcount;
+        if (use >= 1u) {
+          ok = wait_pair(&acc_empty[buf], (use - 1) & 1, failed, p.status);
+          if (!ok) break;
+          tc_fence_after_sync();
+        }
+        uint32_t set = 0;
+        for (int kb = 0; kb < p.Kb; ++kb, ++it) {
+          const int s = it % kStages;
+          if ((kb & 3) == 0) {
+            const int e = g % kSfRing;
+            ok = wait_pair(&sf_full[e], (g / kSfRing) & 1, failed, p.status);
+            if (!ok) break;
+            tc_fence_after_sync();
+            set = tmem + C::kSfCol + (g & 1) * C::kSfCols;
+            if (lane == 0) {
+              const uint32_t src = smem_u32(sf + e * C::kSfBytes);
+#pragma unroll
+              for (int h = 0; h <= C::kSfbBlocks; ++h) xqf8::sf_copy<2>(set + 4 * h, xqf8::sf_desc(src + 512 * h));
+              commit_pair(&sf_empty[e]);
+            }
+            __syncwarp();
+            ++g;
+          }
+          ok = wait_pair(&full[s], (it / kStages) & 1, failed, p.status);
+          if (!ok) break;
+          tc_fence_after_sync();
+          if (lane == 0) {
+            const uint32_t a = smem_u32(base + (size_t)s * kStageBytes);
+            const uint64_t adesc = umma_desc_k128(a), bdesc = umma_desc_k128(a + C::kABytes);
+            const uint32_t id = xqf8::idesc(256, TN, kb & 3);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              xqf8::mma<2>(tmem + buf * TN, adesc + 2 * k, bdesc + 2 * k, id, (kb | k) != 0 ? 1u : 0u, set, set + 4);
+            commit_pair(&empty[s]);
+          }
+          __syncwarp();
+        }
+        if (ok && lane == 0) commit_pair(&acc_full[buf]);
+        __syncwarp();
+      }
+      if (lane == 0) commit_pair(drain);
+      __syncwarp();
+    } else {
+      // follow the leader tile by tile: a wait is never longer than one tile
+      for (int tile = first; tile < tiles && ok; tile += step, ++tcount)
+        ok = wait_pair(&acc_full[kAccBufs == 2 ? tcount & 1 : 0], (kAccBufs == 2 ? tcount >> 1 : tcount) & 1, failed, p.status);
+    }
+    pdl_launch_dependents();
+    wait_pair(drain, 0, failed, p.status);
+  } else if (warp == 2) {
+    // ---- scale words: this CTA's 128 token rows, and the tile's TN weight rows (both CTAs need all of them) ------------
+    pdl_wait();
+    bool ok = true;
+    uint32_t i = 0;
+    for (int tile = first; tile < tiles && ok; tile += step) {
+      const int tm = tile % p.tiles_m, tn = tile / p.tiles_m;
+      const int row_x = tm * 256 + (int)rank * 128;
+      for (int g = 0; 4 * g < p.Kb; ++g, ++i) {
+        const int e = i % kSfRing;
+        if (i >= (uint32_t)kSfRing) {
+          ok = wait_pair(&sf_empty[e], ((i / kSfRing) - 1) & 1, failed, p.status);
+          if (!ok) break;
+        }
+        uint32_t v[4];
+        uint4* dst = reinterpret_cast<uint4*>(sf + e * C::kSfBytes);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int m = row_x + 32 * q + lane;
+          v[q] = m < p.M ? *reinterpret_cast<const uint32_t*>(p.sx + (size_t)m * p.P + 4 * g) : 0x7F7F7F7Fu;
+        }
+        dst[lane] = make_uint4(v[0], v[1], v[2], v[3]);
+#pragma unroll
+        for (int h = 0; h < C::kSfbBlocks; ++h) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            // weight block of columns 128 h + 32 q .. + 31 (a tile starts at a multiple of 64)
+            const int nb = GATED ? tn : (tn * TN + 128 * h + 32 * q) >> 7;
+            v[q] = nb * 128 < p.Np ? *reinterpret_cast<const uint32_t*>(p.sw[GATED ? h : 0] + (size_t)nb * p.P + 4 * g) : 0x7F7F7F7Fu;
+          }
+          dst[32 * (1 + h) + lane] = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) arrive_at(xqf8::map_to(smem_u32(&sf_full[e]), 0));
+      }
+    }
+  } else if (warp >= 4) {
+    // ---- epilogue ---------------------------------------------------------------------------------------------------
+    const int q = warp & 3, half = (warp - 4) >> 2, r = q * 32 + lane;
+    unsigned char* box = outs + (warp - 4) * 2048;
+    float* amax_row = reinterpret_cast<float*>(outs);  // gated 8-bit: [parity][half][128 rows] in the (unused) boxes' memory
+    volatile int* ok_row = reinterpret_cast<volatile int*>(amax_row + 512);
+    uint32_t tcount = 0;
+    bool ok = true;
+    for (int tile = first; tile < tiles && ok; tile += step, ++tcount) {
+      const int tm = tile % p.tiles_m, tn = tile / p.tiles_m;
+      const int m0 = tm * 256 + (int)rank * 128 + q * 32, m = m0 + lane;
+      const uint32_t buf = kAccBufs == 2 ? (tcount & 1u) : 0u, use = kAccBufs == 2 ? tcount >> 1 : tcount;
+      ok = wait_pair(&acc_full[buf], use & 1, failed, p.status);
+      if (GATED && !p.out) {  // the two warps that meet below go on, or stop, together
+        ok_row[(tcount & 1) * 8 + warp - 4] = ok;
+        bar_sync(1 + q, 64);
+        ok = ok && ok_row[(tcount & 1) * 8 + ((warp - 4) ^ 4)];
+      }
+      if (!ok) break;
+      tc_fence_after_sync();
+      const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + buf * TN;
+      auto release = [&] {
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) arrive_at(xqf8::map_to(smem_u32(&acc_empty[buf]), 0));
+      };
+      // 32 columns of this warp's 32 rows -> the warp's box (64-byte rows, 64-byte swizzle) -> global memory
+      auto store32 = [&](const float* v, int nc) {
+        if (p.N % 8 == 0 && lane == 0) bulk_wait_group_read<0>();
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v[8 * c + 2 * e], v[8 * c + 2 * e + 1]);
+            w[e] = *reinterpret_cast<const uint32_t*>(&b);
+          }
+          *reinterpret_cast<uint4*>(box + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        if (p.N % 8 == 0) {
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (nc < p.N && m0 < p.M) tma_store_2d(&map_o, box, nc, m0);
+            bulk_commit_group();
+          }
+        } else {  // rows do not start on 16-byte boundaries: a row per instruction, one element per lane
+          __syncwarp();
+          for (int i = 0; i < 32 && m0 + i < p.M; ++i)
+            if (nc + lane < p.N)
+              p.out[(size_t)(m0 + i) * p.N + nc + lane] =
+                  *reinterpret_cast<const __nv_bfloat16*>(box + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + 2 * (lane & 7));
+        }
+      };
+      if (!GATED) {
+#pragma unroll 1
+        for (int c = 0; c < C::kHalfN / 32; ++c) {
+          uint32_t v[32];
+          tmem_ld_32x32(acc + half * C::kHalfN + 32 * c, v);
+          tmem_ld_wait();
+          if (c == C::kHalfN / 32 - 1) release();
+          store32(reinterpret_cast<const float*>(v), tn * TN + half * C::kHalfN + 32 * c);
+        }
+      } else {
+        uint32_t gv[2][32], uv[2][32];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          tmem_ld_32x32(acc + 64 * half + 32 * c, gv[c]);
+          tmem_ld_32x32(acc + 128 + 64 * half + 32 * c, uv[c]);
+        }
+        tmem_ld_wait();
+        release();
+        float h[2][32], amax = 0.f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int j = 0; j < 32; ++j) h[c][j] = xqf8::silu_mul(__uint_as_float(gv[c][j]), __uint_as_float(uv[c][j]));
+        const int n0 = tn * 128 + 64 * half;
+        if (p.out) {
+          store32(h[0], n0);
+          store32(h[1], n0 + 32);
+        } else {
+          // columns past N have zero weights: G = U = 0 and h = 0
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) amax = fmaxf(amax, fabsf(h[c][j]));
+          float* a = amax_row + (tcount & 1) * 256;
+          a[half * 128 + r] = amax;
+          bar_sync(1 + q, 64);  // with the warp that has the other 64 channels of these rows
+          amax = fmaxf(amax, a[(half ^ 1) * 128 + r]);
+          const int b = xqf8::scale_byte(amax);
+          const float s = xqf8::inv_scale(b);
+          if (m < p.M) {
+            uint8_t* o = p.out_codes + (size_t)m * p.Np + n0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              uint32_t w[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float* x = &h[c >> 1][16 * (c & 1) + 4 * e];
+                w[e] = xqf8::pack4(x[0] * s, x[1] * s, x[2] * s, x[3] * s);
+              }
+              *reinterpret_cast<uint4*>(o + 16 * c) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            if (half == 0) {
+              const int Po = xq_f8_pitch(p.N);
+              uint8_t* os = p.out_scales + (size_t)m * Po + tn;
+              os[0] = (uint8_t)b;
+              if (tn == p.tiles_n - 1)
+                for (int k = 1; tn + k < Po; ++k) os[k] = 127;  // padding of the row's last word
+            }
+          }
+        }
+      }
+    }
+    if (lane == 0) bulk_wait_group<0>();
+    __syncwarp();
+  }
+
+  // neither CTA leaves while the other may still read its shared memory or signal its barriers
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 0 && *failed)
+    for (int s = 0; s < kStages; ++s) mbar_wait(&full[s], 0, 1u << 16), mbar_wait(&full[s], 1, 1u << 16);
+  xqf8::cluster_arrive();
+  xqf8::cluster_wait();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+bool map_2d(CUtensorMap* map, CUtensorMapDataType type, const void* p, uint64_t cols, uint64_t rows, uint64_t pitch_bytes, uint32_t box_cols,
+            uint32_t box_rows, CUtensorMapSwizzle swizzle) {
+  XqEncodeTiledFn enc = xq_encode_tiled_fn();
+  if (!enc) return false;
+  const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch_bytes};
+  const cuuint32_t box[2] = {box_cols, box_rows}, estr[2] = {1, 1};
+  return enc(map, type, 2, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int TN, bool GATED>
+cudaError_t launch(const XqF8GemmArgs& a, cudaStream_t st) {
+  using C = TileCfg<TN>;
+  const xq_f8_weights* w = a.w[0];
+  CUtensorMap map_x, map_w[2], map_o;
+  if (!xq_f8_map_rows(&map_x, a.codes, a.M, w->Kb * 128, 128)) return cudaErrorInvalidValue;
+  // the weights are stored swizzled: plain boxes of whole 128-byte rows
+  for (int h = 0; h < 2; ++h)
+    if (!map_2d(&map_w[h], CU_TENSOR_MAP_DATA_TYPE_UINT8, a.w[GATED ? h : 0]->codes, 128, (uint64_t)w->Kb * w->Np, 128, 128,
+                GATED ? 128 : C::kHalfN, CU_TENSOR_MAP_SWIZZLE_NONE))
+      return cudaErrorInvalidValue;
+  map_o = map_x;  // (not read where rows are not 16-byte multiples, or the result is 8-bit)
+  if (a.out && w->N % 8 == 0 &&
+      !map_2d(&map_o, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.out, w->N, a.M, (uint64_t)w->N * 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+    return cudaErrorInvalidValue;
+  TileParams p;
+  for (int h = 0; h < 2; ++h) p.sw[h] = a.w[GATED ? h : 0]->scales;
+  p.sx = a.scales;
+  p.out = (__nv_bfloat16*)a.out;
+  p.out_codes = a.out_codes;
+  p.out_scales = a.out_scales;
+  p.status = a.status;
+  p.M = a.M;
+  p.N = w->N;
+  p.Np = w->Np;
+  p.Kb = w->Kb;
+  p.P = xq_f8_pitch(w->K);
+  p.tiles_m = (a.M + 255) / 256;
+  p.tiles_n = GATED ? w->Np / 128 : (w->N + TN - 1) / TN;
+  cudaError_t e = cudaFuncSetAttribute(tile_kernel<TN, GATED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemBytes);
+  if (e != cudaSuccess) return e;
+  const int tiles = p.tiles_m * p.tiles_n, pairs = w->sms / 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * (tiles < pairs ? tiles : pairs));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = C::kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, tile_kernel<TN, GATED>, map_x, map_w[0], map_w[1], map_o, p);
+}
+
+}  // namespace
+
+cudaError_t xq_f8_launch_tile(const XqF8GemmArgs& a, int TN, cudaStream_t st) {
+  if (a.w[1]) return launch<256, true>(a, st);
+  if (TN == 128) return launch<128, false>(a, st);
+  if (TN == 192) return launch<192, false>(a, st);
+  return launch<256, false>(a, st);
+}
