@@ -43,6 +43,19 @@ __device__ __forceinline__ void mma(uint32_t d_tmem, uint64_t adesc, uint64_t bd
         : "memory");
 }
 
+// One thread of a converged warp (the same one each time).  The loops that feed the tensor core run in such a thread from
+// beginning to end: branched on inside the loop, or picked by lane number, the operands of every tcgen05 instruction are
+// moved to uniform registers by code that provides for 32 threads, which costs more issue time than the MMAs take.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok));
+  return ok != 0;
+}
+
 // ---- thread-block clusters ---------------------------------------------------------------------------
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }

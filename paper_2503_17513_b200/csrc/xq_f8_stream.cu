@@ -92,68 +92,66 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
 
   if (warp == 0) {
     // ---- producer: the weights do not depend on the kernel before this one, the tokens do -------------------------
-    auto load_weights = [&](int i) {
-      unsigned char* st = base + (size_t)(i % kStages) * kStageBytes;
-      mbar_expect_tx(&full[i % kStages], kStageBytes);
+    if (xqf8::elect_one()) {
+      auto load_weights = [&](int kb, int s) {
+        unsigned char* st = base + (size_t)s * kStageBytes;
+        mbar_expect_tx(&full[s], kStageBytes);
 #pragma unroll
-      for (int h = 0; h < MATS; ++h)
-        bulk_g2s(st + h * 16384, p.w[h] + ((size_t)(kb_lo + i) * p.Np + (size_t)tile * 128) * 128, 16384, &full[i % kStages]);
-    };
-    const int pre = nk < kStages ? nk : kStages;
-    if (lane == 0)
-      for (int i = 0; i < pre; ++i) load_weights(i);
-    __syncwarp();
-    pdl_wait();
-    for (int i = 0; i < nk; ++i) {
-      const int s = i % kStages;
-      if (i >= kStages && !mbar_wait_bounded(&empty[s], ((i / kStages) - 1) & 1, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
-      if (lane == 0) {
-        if (i >= kStages) load_weights(i);
-        tma_load_2d(base + (size_t)s * kStageBytes + MATS * 16384, &map_x, (kb_lo + i) * 128, t0, &full[s]);
+        for (int h = 0; h < MATS; ++h) bulk_g2s(st + h * 16384, p.w[h] + ((size_t)kb * p.Np + (size_t)tile * 128) * 128, 16384, &full[s]);
+      };
+      auto load_tokens = [&](int kb, int s) {
+        tma_load_2d(base + (size_t)s * kStageBytes + MATS * 16384, &map_x, kb * 128, t0, &full[s]);
+      };
+      const int pre = nk < kStages ? nk : kStages;
+      for (int i = 0; i < pre; ++i) load_weights(kb_lo + i, i);
+      pdl_wait();
+      for (int i = 0; i < pre; ++i) load_tokens(kb_lo + i, i);
+      int s = 0;
+      uint32_t phase = 0;
+      for (int kb = kb_lo + pre; kb < kb_hi; ++kb) {
+        if (!mbar_wait_bounded(&empty[s], phase, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
+        load_weights(kb, s);
+        load_tokens(kb, s);
+        if (++s == kStages) s = 0, phase ^= 1;
       }
-      __syncwarp();
     }
+    __syncwarp();
   } else if (warp == 1) {
     // ---- MMA issue ------------------------------------------------------------------------------------------
-    bool ok = true;
-    uint32_t set = 0;
-    for (int i = 0, g = -1; i < nk; ++i) {
-      const int s = i % kStages, kb = kb_lo + i;
-      if (i == 0 || (kb & 3) == 0) {  // the next scale words
-        ++g;
-        ok = mbar_wait_bounded(&sf_full[g % kSfRing], (g / kSfRing) & 1, failed, p.status, (int)XQ_ERR_TIMEOUT);
-        if (!ok) break;
-        tc_fence_after_sync();
-        // two sets of columns in turn: a copy never lands under an instruction that still reads the set before
-        set = tmem + C::kSfCol + (g & 1) * (MATS + 1) * 4;
-        if (lane == 0) {
-          const uint32_t src = smem_u32(sf + (g % kSfRing) * C::kSfBytes);
+    if (xqf8::elect_one()) {
+      const uint64_t adesc0 = umma_desc_k128(smem_u32(base)), sfdesc0 = xqf8::sf_desc(smem_u32(sf));
+      const uint32_t id0 = xqf8::idesc(128, NT, 0), id_step = xqf8::idesc(128, NT, 1) - id0;
+      int s = 0, e = 0;
+      uint32_t phase = 0, sf_phase = 0, sf_set = 0, set = 0, accumulate = 0;
+      for (int kb = kb_lo; kb < kb_hi; ++kb) {
+        if (kb == kb_lo || (kb & 3) == 0) {  // the next scale words
+          if (!mbar_wait_bounded(&sf_full[e], sf_phase, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
+          tc_fence_after_sync();
+          // two sets of columns in turn: a copy never lands under an instruction that still reads the set before
+          set = tmem + C::kSfCol + sf_set * (MATS + 1) * 4;
+          sf_set ^= 1;
 #pragma unroll
-          for (int h = 0; h <= MATS; ++h) xqf8::sf_copy<1>(set + 4 * h, xqf8::sf_desc(src + 512 * h));
-          umma_commit(&sf_empty[g % kSfRing]);
+          for (int h = 0; h <= MATS; ++h) xqf8::sf_copy<1>(set + 4 * h, sfdesc0 + (uint64_t)((e * C::kSfBytes + 512 * h) >> 4));
+          umma_commit(&sf_empty[e]);
+          if (++e == kSfRing) e = 0, sf_phase ^= 1;
         }
-        __syncwarp();
-      }
-      ok = mbar_wait_bounded(&full[s], (i / kStages) & 1, failed, p.status, (int)XQ_ERR_TIMEOUT);
-      if (!ok) break;
-      tc_fence_after_sync();
-      if (lane == 0) {
-        const uint32_t a = smem_u32(base + (size_t)s * kStageBytes);
-        const uint64_t bdesc = umma_desc_k128(a + MATS * 16384);
-        const uint32_t id = xqf8::idesc(128, NT, kb & 3);
+        if (!mbar_wait_bounded(&full[s], phase, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
+        tc_fence_after_sync();
+        const uint64_t adesc = adesc0 + (uint64_t)((s * kStageBytes) >> 4), bdesc = adesc + (MATS * 16384 >> 4);
+        const uint32_t id = id0 + (kb & 3) * id_step;
 #pragma unroll
-        for (int h = 0; h < MATS; ++h) {
-          const uint64_t adesc = umma_desc_k128(a + h * 16384);
+        for (int k = 0; k < 4; ++k) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            xqf8::mma<1>(tmem + h * NT, adesc + 2 * k, bdesc + 2 * k, id, (i | k) != 0 ? 1u : 0u, set + 4 * (1 + h), set);
+          for (int h = 0; h < MATS; ++h)
+            xqf8::mma<1>(tmem + h * NT, adesc + (h * 16384 >> 4) + 2 * k, bdesc + 2 * k, id, accumulate, set + 4 * (1 + h), set);
+          accumulate = 1;
         }
         umma_commit(&empty[s]);
+        if (++s == kStages) s = 0, phase ^= 1;
       }
-      __syncwarp();
+      // after a failed wait this still signals once everything issued is over, so that nothing is in flight at the end
+      umma_commit(acc_full);
     }
-    // after a failed wait this still signals once everything issued is over, so that nothing is in flight at the end
-    if (lane == 0) umma_commit(acc_full);
     __syncwarp();
   } else if (warp == 2) {
     // ---- scale words: block 0 the tokens', then one block per weight matrix (one word: all 128 channels share it) ----

@@ -71,6 +71,10 @@ __device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, volati
   atomicExch(status, (int)XQ_ERR_TIMEOUT);
   return false;
 }
+// A wait for copies or for the tensor core: their completion is what makes the data visible.
+__device__ __forceinline__ bool wait_cta(uint64_t* bar, uint32_t parity, volatile int* failed, int* status) {
+  return mbar_wait_bounded(bar, parity, failed, status, (int)XQ_ERR_TIMEOUT);
+}
 // arrival on a barrier anywhere in the pair (address from map_to)
 __device__ __forceinline__ void arrive_at(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -140,84 +144,84 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == 0) {
     // ---- loads: this CTA's 128 token rows and its half of the weight rows ------------------------------------------
     pdl_wait();
-    const void* map_w = rank && GATED ? (const void*)&map_w1 : (const void*)&map_w0;
-    bool ok = true;
-    uint32_t it = 0;
-    for (int tile = first; tile < tiles && ok; tile += step) {
-      const int tm = tile % p.tiles_m, tn = tile / p.tiles_m;
-      const int row_x = tm * 256 + (int)rank * 128, row_w = GATED ? tn * 128 : tn * TN + (int)rank * C::kHalfN;
-      for (int kb = 0; kb < p.Kb; ++kb, ++it) {
-        const int s = it % kStages;
-        if (it >= (uint32_t)kStages) {
-          ok = wait_pair(&empty[s], ((it / kStages) - 1) & 1, failed, p.status);
+    if (xqf8::elect_one()) {
+      const void* map_w = rank && GATED ? (const void*)&map_w1 : (const void*)&map_w0;
+      const uint32_t full0 = xqf8::map_to(smem_u32(full), 0);  // the leader's barriers
+      bool ok = true;
+      int s = 0;
+      uint32_t phase = 1;  // the first pass over the ring finds it empty
+      for (int tile = first; tile < tiles && ok; tile += step) {
+        const int tm = tile % p.tiles_m, tn = tile / p.tiles_m;
+        const int row_x = tm * 256 + (int)rank * 128;
+        int row_w = GATED ? tn * 128 : tn * TN + (int)rank * C::kHalfN;
+        for (int kb = 0; kb < p.Kb; ++kb, row_w += p.Np) {
+          ok = wait_cta(&empty[s], phase, failed, p.status);
           if (!ok) break;
-        }
-        if (lane == 0) {
           unsigned char* st = base + (size_t)s * kStageBytes;
-          const uint32_t bar = xqf8::map_to(smem_u32(&full[s]), 0);
           if (rank == 0) mbar_expect_tx(&full[s], 2 * kStageBytes);  // both CTAs' copies
-          load_pair(st, &map_x, kb * 128, row_x, bar);
-          load_pair(st + C::kABytes, map_w, 0, kb * p.Np + row_w, bar);
+          load_pair(st, &map_x, kb * 128, row_x, full0 + 8 * s);
+          load_pair(st + C::kABytes, map_w, 0, row_w, full0 + 8 * s);
+          if (++s == kStages) s = 0, phase ^= 1;
         }
-        __syncwarp();
       }
     }
+    __syncwarp();
   } else if (warp == 1) {
     // ---- MMA issue (the leader, for both) ------------------------------------------------------------------------
     bool ok = true;
-    uint32_t it = 0, g = 0, tcount = 0;
     if (rank == 0) {
-      for (int tile = first; tile < tiles && ok; tile += step, ++tcount) {
-        const uint32_t buf = kAccBufs == 2 ? (tcount & 1u) : 0u, use = kAccBufs == 2 ? tcount >> 1 : tcount;
-        if (use >= 1u) {
-          ok = wait_pair(&acc_empty[buf], (use - 1) & 1, failed, p.status);
+      if (xqf8::elect_one()) {
+        const uint64_t adesc0 = umma_desc_k128(smem_u32(base)), bdesc0 = umma_desc_k128(smem_u32(base) + C::kABytes);
+        const uint64_t sfdesc0 = xqf8::sf_desc(smem_u32(sf));
+        const uint32_t id0 = xqf8::idesc(256, TN, 0), id_step = xqf8::idesc(256, TN, 1) - id0;
+        int s = 0, e = 0;
+        uint32_t phase = 0, sf_phase = 0, sf_set = 0, tcount = 0;
+        for (int tile = first; tile < tiles && ok; tile += step, ++tcount) {
+          const uint32_t buf = kAccBufs == 2 ? (tcount & 1u) : 0u, use = kAccBufs == 2 ? tcount >> 1 : tcount;
+          ok = wait_pair(&acc_empty[buf], (use & 1) ^ 1, failed, p.status);  // (the first use finds it free)
           if (!ok) break;
           tc_fence_after_sync();
-        }
-        uint32_t set = 0;
-        for (int kb = 0; kb < p.Kb; ++kb, ++it) {
-          const int s = it % kStages;
-          if ((kb & 3) == 0) {
-            const int e = g % kSfRing;
-            ok = wait_pair(&sf_full[e], (g / kSfRing) & 1, failed, p.status);
+          const uint32_t acc = tmem + buf * TN;
+          uint32_t set = 0, accumulate = 0;
+          for (int kb = 0; kb < p.Kb; ++kb) {
+            if ((kb & 3) == 0) {
+              ok = wait_pair(&sf_full[e], sf_phase, failed, p.status);
+              if (!ok) break;
+              tc_fence_after_sync();
+              // two sets of columns in turn: a copy never lands under an instruction that still reads the set before
+              set = tmem + C::kSfCol + sf_set * C::kSfCols;
+              sf_set ^= 1;
+#pragma unroll
+              for (int h = 0; h <= C::kSfbBlocks; ++h) xqf8::sf_copy<2>(set + 4 * h, sfdesc0 + (uint64_t)((e * C::kSfBytes + 512 * h) >> 4));
+              commit_pair(&sf_empty[e]);
+              if (++e == kSfRing) e = 0, sf_phase ^= 1;
+            }
+            ok = wait_cta(&full[s], phase, failed, p.status);
             if (!ok) break;
             tc_fence_after_sync();
-            set = tmem + C::kSfCol + (g & 1) * C::kSfCols;
-            if (lane == 0) {
-              const uint32_t src = smem_u32(sf + e * C::kSfBytes);
+            const uint64_t adesc = adesc0 + (uint64_t)((s * kStageBytes) >> 4), bdesc = bdesc0 + (uint64_t)((s * kStageBytes) >> 4);
+            const uint32_t id = id0 + (kb & 3) * id_step;
 #pragma unroll
-              for (int h = 0; h <= C::kSfbBlocks; ++h) xqf8::sf_copy<2>(set + 4 * h, xqf8::sf_desc(src + 512 * h));
-              commit_pair(&sf_empty[e]);
+            for (int k = 0; k < 4; ++k) {
+              xqf8::mma<2>(acc, adesc + 2 * k, bdesc + 2 * k, id, accumulate, set, set + 4);
+              accumulate = 1;
             }
-            __syncwarp();
-            ++g;
-          }
-          ok = wait_pair(&full[s], (it / kStages) & 1, failed, p.status);
-          if (!ok) break;
-          tc_fence_after_sync();
-          if (lane == 0) {
-            const uint32_t a = smem_u32(base + (size_t)s * kStageBytes);
-            const uint64_t adesc = umma_desc_k128(a), bdesc = umma_desc_k128(a + C::kABytes);
-            const uint32_t id = xqf8::idesc(256, TN, kb & 3);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              xqf8::mma<2>(tmem + buf * TN, adesc + 2 * k, bdesc + 2 * k, id, (kb | k) != 0 ? 1u : 0u, set, set + 4);
             commit_pair(&empty[s]);
+            if (++s == kStages) s = 0, phase ^= 1;
           }
-          __syncwarp();
+          if (ok) commit_pair(&acc_full[buf]);
         }
-        if (ok && lane == 0) commit_pair(&acc_full[buf]);
-        __syncwarp();
+        commit_pair(drain);
       }
-      if (lane == 0) commit_pair(drain);
       __syncwarp();
     } else {
       // follow the leader tile by tile: a wait is never longer than one tile
+      uint32_t tcount = 0;
       for (int tile = first; tile < tiles && ok; tile += step, ++tcount)
-        ok = wait_pair(&acc_full[kAccBufs == 2 ? tcount & 1 : 0], (kAccBufs == 2 ? tcount >> 1 : tcount) & 1, failed, p.status);
+        ok = wait_cta(&acc_full[kAccBufs == 2 ? tcount & 1 : 0], (kAccBufs == 2 ? tcount >> 1 : tcount) & 1, failed, p.status);
     }
     pdl_launch_dependents();
-    wait_pair(drain, 0, failed, p.status);
+    wait_cta(drain, 0, failed, p.status);
   } else if (warp == 2) {
     // ---- scale words: this CTA's 128 token rows, and the tile's TN weight rows (both CTAs need all of them) ------------
     pdl_wait();
@@ -229,7 +233,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (int g = 0; 4 * g < p.Kb; ++g, ++i) {
         const int e = i % kSfRing;
         if (i >= (uint32_t)kSfRing) {
-          ok = wait_pair(&sf_empty[e], ((i / kSfRing) - 1) & 1, failed, p.status);
+          ok = wait_cta(&sf_empty[e], ((i / kSfRing) - 1) & 1, failed, p.status);
           if (!ok) break;
         }
         uint32_t v[4];
@@ -267,7 +271,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int tm = tile % p.tiles_m, tn = tile / p.tiles_m;
       const int m0 = tm * 256 + (int)rank * 128 + q * 32, m = m0 + lane;
       const uint32_t buf = kAccBufs == 2 ? (tcount & 1u) : 0u, use = kAccBufs == 2 ? tcount >> 1 : tcount;
-      ok = wait_pair(&acc_full[buf], use & 1, failed, p.status);
+      ok = wait_cta(&acc_full[buf], use & 1, failed, p.status);
       if (GATED && !p.out) {  // the two warps that meet below go on, or stop, together
         ok_row[(tcount & 1) * 8 + warp - 4] = ok;
         bar_sync(1 + q, 64);
