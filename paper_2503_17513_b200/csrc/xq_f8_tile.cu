@@ -315,14 +315,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       };
       if (!GATED) {
-#pragma unroll 1
-        for (int c = 0; c < C::kHalfN / 32; ++c) {
-          uint32_t v[32];
-          tmem_ld_32x32(acc + half * C::kHalfN + 32 * c, v);
-          tmem_ld_wait();
-          if (c == C::kHalfN / 32 - 1) release();
-          store32(reinterpret_cast<const float*>(v), tn * TN + half * C::kHalfN + 32 * c);
-        }
+        // all of the warp's columns into registers first: with one accumulator, the next tile's MMAs wait for this
+        uint32_t v[C::kHalfN / 32][32];
+#pragma unroll
+        for (int c = 0; c < C::kHalfN / 32; ++c) tmem_ld_32x32(acc + half * C::kHalfN + 32 * c, v[c]);
+        tmem_ld_wait();
+        release();
+#pragma unroll
+        for (int c = 0; c < C::kHalfN / 32; ++c)
+          store32(reinterpret_cast<const float*>(v[c]), tn * TN + half * C::kHalfN + 32 * c);
       } else {
         uint32_t gv[2][32], uv[2][32];
 #pragma unroll
