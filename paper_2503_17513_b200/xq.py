@@ -553,47 +553,78 @@ def new_f8_workspace(M_max: int, w: F8Weights, device="cuda") -> torch.Tensor:
     return ws
 
 
-def _rows(t):
-    """(address, row pitch) of a 2-D device tensor whose rows are contiguous; (null, 0) for None."""
-    if t is None:
-        return ctypes.c_void_p(0), 0
-    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)
-    return ctypes.c_void_p(t.data_ptr()), t.stride(0)
+# The calls below are what a decoding loop makes once per layer and token, where the host's time counts: pointers go over as
+# plain integers and the stream is read by its handle (2 us a call instead of 9 with the wrappers above).
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _rows(t) -> int:
+    """Row pitch of a 2-D device tensor whose rows are contiguous."""
+    assert t.is_cuda and t.dim() == 2
+    ld, step = t.stride()
+    assert step == 1 or t.shape[1] == 1
+    return ld
+
+
+def _flat(t) -> int:
+    """Address of a contiguous device tensor."""
+    assert t.is_cuda and t.is_contiguous()
+    return t.data_ptr()
+
+
+def _on(stream, t) -> int:
+    """Handle of `stream`, or of the current stream of t's device."""
+    return _raw_stream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def xq_f8_quant(X, codes, scales, stream=None) -> None:
-    p, ldx = _rows(X)
-    _check(lib().xq_f8_quant(p, X.shape[0], X.shape[1], ldx, _dp(codes), _dp(scales), _stream(stream)), "xq_f8_quant")
+    ldx = _rows(X)
+    M, K = X.shape
+    st = lib().xq_f8_quant(X.data_ptr(), M, K, ldx, _flat(codes), _flat(scales), _on(stream, X))
+    if st:
+        raise XqError(st, "xq_f8_quant")
 
 
 def xq_f8_norm_quant(X, gamma, eps: float, codes, scales, residual=None, sum_out=None, y=None, stream=None) -> None:
     """residual and sum_out may be the same tensor; if both are given their row pitches must be equal."""
-    p, ldx = _rows(X)
-    rp, ldr = _rows(residual)
-    sp, lds = _rows(sum_out)
-    yp, ldy = _rows(y)
-    M, K = X.shape
-    assert residual is None or sum_out is None or ldr == lds
-    for t in (residual, sum_out, y):
-        assert t is None or t.shape == X.shape
+    ldx, shape = _rows(X), X.shape
+    M, K = shape
+    rp = sp = yp = None
+    ldr = ldy = 0
+    if residual is not None:
+        ldr, rp = _rows(residual), residual.data_ptr()
+        assert residual.shape == shape
+    if sum_out is not None:
+        lds, sp = _rows(sum_out), sum_out.data_ptr()
+        assert sum_out.shape == shape and (residual is None or lds == ldr)
+        ldr = lds
+    if y is not None:
+        ldy, yp = _rows(y), y.data_ptr()
+        assert y.shape == shape
     assert gamma.numel() == K
-    _check(lib().xq_f8_norm_quant(p, M, K, ldx, rp, ldr or lds, _dp(gamma), eps, sp, _dp(codes), _dp(scales), yp, ldy, _stream(stream)),
-           "xq_f8_norm_quant")
+    st = lib().xq_f8_norm_quant(X.data_ptr(), M, K, ldx, rp, ldr, _flat(gamma), eps, sp, _flat(codes), _flat(scales), yp, ldy, _on(stream, X))
+    if st:
+        raise XqError(st, "xq_f8_norm_quant")
 
 
 def xq_f8_gemm(codes, scales, M: int, w: F8Weights, out, ws, stream=None) -> None:
-    _check(lib().xq_f8_gemm(_dp(codes), _dp(scales), M, w.handle, _dp(out), _dp(ws), ws.numel() * ws.element_size(), _stream(stream)),
-           "xq_f8_gemm")
+    st = lib().xq_f8_gemm(_flat(codes), _flat(scales), M, w.handle, None if out is None else _flat(out), _flat(ws), ws.nbytes, _on(stream, ws))
+    if st:
+        raise XqError(st, "xq_f8_gemm")
 
 
 def xq_f8_linear(X, w: F8Weights, out, ws, M=None, ldx=None, stream=None) -> None:
     M = X.shape[0] if M is None else M
     ldx = X.stride(0) if ldx is None else ldx
-    _check(lib().xq_f8_linear(ctypes.c_void_p(X.data_ptr()), M, ldx, w.handle, _dp(out), _dp(ws), ws.numel() * ws.element_size(),
-                              _stream(stream)), "xq_f8_linear")
+    st = lib().xq_f8_linear(X.data_ptr(), M, ldx, w.handle, _flat(out), _flat(ws), ws.nbytes, _on(stream, ws))
+    if st:
+        raise XqError(st, "xq_f8_linear")
 
 
 def xq_f8_gated(codes, scales, M: int, gate: F8Weights, up: F8Weights, ws, out=None, out_codes=None, out_scales=None, stream=None) -> None:
     """silu(tokens x gate^T) * (tokens x up^T): bf16 rows into `out`, or 8-bit rows into `out_codes` and `out_scales`."""
-    _check(lib().xq_f8_gated(_dp(codes), _dp(scales), M, gate.handle, up.handle, _dp(out), _dp(out_codes), _dp(out_scales), _dp(ws),
-                             ws.numel() * ws.element_size(), _stream(stream)), "xq_f8_gated")
+    st = lib().xq_f8_gated(_flat(codes), _flat(scales), M, gate.handle, up.handle, None if out is None else _flat(out),
+                           None if out_codes is None else _flat(out_codes), None if out_scales is None else _flat(out_scales), _flat(ws),
+                           ws.nbytes, _on(stream, ws))
+    if st:
+        raise XqError(st, "xq_f8_gated")
