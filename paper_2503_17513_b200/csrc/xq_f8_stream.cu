@@ -30,28 +30,25 @@ struct StreamParams {
 constexpr int kThreads = 7 * 32;
 constexpr int kSfRing = 4;  // scale words of four K blocks each, in shared memory
 
-// NT: token columns of a tile; MATS: 1, or 2 for the gated pair
-template <int NT, int MATS>
+// NT: token columns of a tile; MATS: 1, or 2 for the gated pair; PER_SM: CTAs that share a multiprocessor
+template <int NT, int MATS, int PER_SM>
 struct StreamCfg {
   static constexpr int kStageBytes = MATS * 16384 + NT * 128;
   static constexpr int kSfBytes = (MATS + 1) * 512;
-  // two CTAs on a multiprocessor (113 KiB each) where three stages fit, else one
-  static constexpr int kHalf = 113 * 1024 - 2048 - kSfRing * kSfBytes, kWhole = 226 * 1024 - 2048 - kSfRing * kSfBytes;
-  static constexpr int kPerSm = kHalf / kStageBytes >= 3 ? 2 : 1;
-  static constexpr int kBudget = kPerSm == 2 ? kHalf : kWhole;
-  static constexpr int kStages = kBudget / kStageBytes < 8 ? kBudget / kStageBytes : 8;
-  static constexpr int kRedBytes = MATS * 512 * (NT + 7);  // partial tiles (S * ceil(NT / S) <= NT + 7 columns), in the stages' memory
+  static constexpr int kBudget = (PER_SM == 2 ? 113 : 226) * 1024 - 2048 - kSfRing * kSfBytes;
+  static constexpr int kStages = kBudget / kStageBytes < 12 ? kBudget / kStageBytes : 12;
+  static constexpr int kRedBytes = MATS * 2048 * (NT / 4 + 7);  // partial tiles (S * ceil(NT / 4 / S) <= NT / 4 + 7 units)
   static constexpr int kAccCols = MATS * NT;
-  static constexpr int kSfCol = kAccCols;                // two sets of (MATS + 1) * 4 columns
+  static constexpr int kSfCol = kAccCols;                       // two sets of (MATS + 1) * 4 columns
   static constexpr int kNeed = kAccCols + 2 * (MATS + 1) * 4;
   static constexpr int kTmemCols = kNeed <= 64 ? 64 : kNeed <= 128 ? 128 : kNeed <= 256 ? 256 : 512;
-  static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kSfRing * kSfBytes + 256;
+  static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kSfRing * kSfBytes + 512;
   static_assert(kStages >= 3 && kStages * kStageBytes >= kRedBytes, "stages hold the partial tiles");
 };
 
-template <int NT, int MATS>
+template <int NT, int MATS, int PER_SM>
 __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant__ CUtensorMap map_x, const StreamParams p) {
-  using C = StreamCfg<NT, MATS>;
+  using C = StreamCfg<NT, MATS, PER_SM>;
   constexpr int kStages = C::kStages, kStageBytes = C::kStageBytes;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -72,38 +69,43 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
   const int nk = kb_hi - kb_lo;
   const int g_lo = kb_lo >> 2, g_hi = (kb_hi + 3) >> 2;                           // its scale words
 
-  if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
-    for (int s = 0; s < kSfRing; ++s) mbar_init(&sf_full[s], 1), mbar_init(&sf_empty[s], 1);
-    mbar_init(acc_full, 1);
-    *failed = 0;
-    mbar_fence_init();
-    tma_prefetch_desc(&map_x);
-  }
-  if (warp == 1) {
+  auto load_weights = [&](int kb, int s) {
+    unsigned char* st = base + (size_t)s * kStageBytes;
+    mbar_expect_tx(&full[s], kStageBytes);
+#pragma unroll
+    for (int h = 0; h < MATS; ++h) bulk_g2s(st + h * 16384, p.w[h] + ((size_t)kb * p.Np + (size_t)tile * 128) * 128, 16384, &full[s]);
+  };
+  const int pre = nk < kStages ? nk : kStages;
+  pdl_launch_dependents();
+  if (warp == 0) {
+    // the weights do not depend on the kernel before this one: the first of them are under way before anything else is set up
+    if (xqf8::elect_one()) {
+      for (int s = 0; s < kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
+      mbar_fence_init();
+      for (int i = 0; i < pre; ++i) load_weights(kb_lo + i, i);
+      for (int s = 0; s < kSfRing; ++s) mbar_init(&sf_full[s], 1), mbar_init(&sf_empty[s], 1);
+      mbar_init(acc_full, 1);
+      *failed = 0;
+      mbar_fence_init();
+    }
+    __syncwarp();
+  } else if (warp == 1) {
     tmem_alloc(tmem_slot, C::kTmemCols);
     tmem_relinquish();
+  } else if (tid == 64) {
+    tma_prefetch_desc(&map_x);
   }
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
-  pdl_launch_dependents();
 
   if (warp == 0) {
-    // ---- producer: the weights do not depend on the kernel before this one, the tokens do -------------------------
+    // ---- producer: tokens once the kernel before this one is done, then both as stages come free --------------------
     if (xqf8::elect_one()) {
-      auto load_weights = [&](int kb, int s) {
-        unsigned char* st = base + (size_t)s * kStageBytes;
-        mbar_expect_tx(&full[s], kStageBytes);
-#pragma unroll
-        for (int h = 0; h < MATS; ++h) bulk_g2s(st + h * 16384, p.w[h] + ((size_t)kb * p.Np + (size_t)tile * 128) * 128, 16384, &full[s]);
-      };
       auto load_tokens = [&](int kb, int s) {
         tma_load_2d(base + (size_t)s * kStageBytes + MATS * 16384, &map_x, kb * 128, t0, &full[s]);
       };
-      const int pre = nk < kStages ? nk : kStages;
-      for (int i = 0; i < pre; ++i) load_weights(kb_lo + i, i);
       pdl_wait();
       for (int i = 0; i < pre; ++i) load_tokens(kb_lo + i, i);
       int s = 0;
@@ -178,10 +180,10 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
     }
   }
 
-  // ---- partial tiles to the CTAs that own their tokens: token c belongs to slice c mod S, slot c / S --------------------
-  // [matrix][slice][slot][128 channels] fp32 in the owner's stage memory; every CTA of the cluster must be done with its stages
-  float* red = reinterpret_cast<float*>(base);
-  const int slots = (NT + S - 1) / S;
+  // ---- partial tiles to the CTAs that own their tokens ---------------------------------------------------------------
+  // Four tokens x 128 channels are a unit (2 KiB: 16 bytes per channel); unit u belongs to slice u mod S, slot u / S.
+  // [matrix][slice][slot][unit] in the owner's stage memory: every CTA of the cluster has to be done with its stages first.
+  const int units = (mt + 3) >> 2, slots = (units + S - 1) / S;
   if (warp >= 3) mbar_wait_bounded(acc_full, 0, failed, p.status, (int)XQ_ERR_TIMEOUT);
   __syncwarp();
   if (S > 1) {
@@ -191,20 +193,20 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
   if (warp >= 3) {
     const int q = warp & 3;
     tc_fence_after_sync();
-    const uint32_t mine = smem_u32(red) + 4 * (q * 32 + lane);
+    const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16), mine = smem_u32(base) + 16 * (q * 32 + lane);
 #pragma unroll 1
     for (int h = 0; h < MATS; ++h) {
+      int owner = 0, slot = (h * S + rank) * slots;
 #pragma unroll 1
-      for (int c0 = 0; c0 < mt; c0 += 16) {
+      for (int u0 = 0; u0 < units; u0 += 4) {
         uint32_t v[16];
-        tmem_ld_32x16(tmem + ((uint32_t)(q * 32) << 16) + h * NT + c0, v);
+        tmem_ld_32x16(lanes + h * NT + 4 * u0, v);
         tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int c = c0 + j;
-          if (c < mt) {
-            const uint32_t at = mine + 512u * (uint32_t)((h * S + rank) * slots + c / S);
-            xqf8::st_cluster(xqf8::map_to(at, c % S), __uint_as_float(v[j]));
+        for (int j = 0; j < 4; ++j) {
+          if (u0 + j < units) {
+            xqf8::st_cluster(xqf8::map_to(mine + 2048u * (uint32_t)slot, owner), make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+            if (++owner == S) owner = 0, ++slot;
           }
         }
       }
@@ -218,45 +220,53 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
   } else {
     __syncthreads();
   }
-  // ---- a warp per token: lane = four channels ------------------------------------------------------------------------
-  const int n = tile * 128 + 4 * lane;
-  for (int slot = warp; slot * S + rank < mt; slot += kThreads / 32) {
-    const size_t m = (size_t)t0 + slot * S + rank;
-    float v[MATS][4] = {};
+  // ---- a warp per unit: lane = channels lane, lane + 32, lane + 64, lane + 96 of four tokens -----------------------------
+  const int n = tile * 128 + lane;
+  for (int slot = warp; slot * S + rank < units; slot += kThreads / 32) {
+    const int c = 4 * (slot * S + rank);  // first token of the unit, within the tile
+    float v[MATS][4][4];                  // [matrix][channel][token]
 #pragma unroll
-    for (int h = 0; h < MATS; ++h)
-      for (int s = 0; s < S; ++s) {
-        const float4 t = *reinterpret_cast<const float4*>(red + ((h * S + s) * slots + slot) * 128 + 4 * lane);
-        v[h][0] += t.x, v[h][1] += t.y, v[h][2] += t.z, v[h][3] += t.w;
+    for (int h = 0; h < MATS; ++h) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[h][i][j] = 0.f;
+      for (int s = 0; s < S; ++s) {  // in slice order
+        const float4* src = reinterpret_cast<const float4*>(base + 2048 * (size_t)((h * S + s) * slots + slot));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 t = src[32 * i + lane];
+          v[h][i][0] += t.x, v[h][i][1] += t.y, v[h][i][2] += t.z, v[h][i][3] += t.w;
+        }
       }
+    }
     if (MATS == 2) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[0][j] = xqf8::silu_mul(v[0][j], v[MATS - 1][j]);
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[0][i][j] = xqf8::silu_mul(v[0][i][j], v[MATS - 1][i][j]);
     }
-    if (MATS == 1 || p.out) {
-      __nv_bfloat16* o = p.out + m * p.N + n;
-      if (n + 4 <= p.N && p.N % 4 == 0) {
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0][0], v[0][1]), hi = __floats2bfloat162_rn(v[0][2], v[0][3]);
-        *reinterpret_cast<uint2*>(o) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (c + j >= mt) break;
+      const size_t m = (size_t)t0 + c + j;
+      if (MATS == 1 || p.out) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n + 32 * i < p.N) p.out[m * p.N + n + 32 * i] = __float2bfloat16_rn(v[0][i][j]);
       } else {
+        // columns past N have zero weights: G = U = 0 and h = 0
+        float a = fmaxf(fmaxf(fabsf(v[0][0][j]), fabsf(v[0][1][j])), fmaxf(fabsf(v[0][2][j]), fabsf(v[0][3][j])));
+        for (int o = 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+        const int b = xqf8::scale_byte(a);
+        const float sc = xqf8::inv_scale(b);
+        const uint32_t w = xqf8::pack4(v[0][0][j] * sc, v[0][1][j] * sc, v[0][2][j] * sc, v[0][3][j] * sc);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (n + j < p.N) o[j] = __float2bfloat16_rn(v[0][j]);
+        for (int i = 0; i < 4; ++i) p.out_codes[m * p.Np + n + 32 * i] = (uint8_t)(w >> (8 * i));
+        const int Po = xq_f8_pitch(p.N);
+        if (lane == 0) p.out_scales[m * Po + tile] = (uint8_t)b;
+        if (tile == p.Np / 128 - 1 && lane > 0 && tile + lane < Po) p.out_scales[m * Po + tile + lane] = 127;  // the row's last word
       }
-    } else {
-      float a = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (n + j >= p.N) v[0][j] = 0.f;
-        a = fmaxf(a, fabsf(v[0][j]));
-      }
-      for (int o = 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-      const int b = xqf8::scale_byte(a);
-      const float sc = xqf8::inv_scale(b);
-      *reinterpret_cast<uint32_t*>(p.out_codes + m * p.Np + n) = xqf8::pack4(v[0][0] * sc, v[0][1] * sc, v[0][2] * sc, v[0][3] * sc);
-      const int Po = xq_f8_pitch(p.N), Gn = p.Np / 128;
-      if (lane == 0) p.out_scales[m * Po + tile] = (uint8_t)b;
-      if (tile == Gn - 1 && lane > 0 && tile + lane < Po) p.out_scales[m * Po + tile + lane] = 127;  // padding of the row's last word
     }
   }
   __syncthreads();
@@ -268,9 +278,9 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
   }
 }
 
-template <int NT, int MATS>
-cudaError_t launch(const XqF8GemmArgs& a, cudaStream_t st) {
-  using C = StreamCfg<NT, MATS>;
+template <int NT, int MATS, int PER_SM>
+cudaError_t launch(const XqF8GemmArgs& a, int S, cudaStream_t st) {
+  using C = StreamCfg<NT, MATS, PER_SM>;
   const xq_f8_weights* w = a.w[0];
   CUtensorMap map_x;
   if (!xq_f8_map_rows(&map_x, a.codes, a.M, w->Kb * 128, NT)) return cudaErrorInvalidValue;
@@ -286,14 +296,11 @@ cudaError_t launch(const XqF8GemmArgs& a, cudaStream_t st) {
   p.Np = w->Np;
   p.Kb = w->Kb;
   p.P = xq_f8_pitch(w->K);
-  const int tiles = w->Np / 128, rows = (a.M + NT - 1) / NT, slots = w->sms * C::kPerSm;
-  int S = 1;
-  while (S < 8 && (S + 1) * tiles * rows <= slots && (S + 1) * 2 <= w->Kb) ++S;
   p.S = S;
-  cudaError_t e = cudaFuncSetAttribute(stream_kernel<NT, MATS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemBytes);
+  cudaError_t e = cudaFuncSetAttribute(stream_kernel<NT, MATS, PER_SM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemBytes);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(tiles * S, rows);
+  cfg.gridDim = dim3(w->Np / 128 * S, (a.M + NT - 1) / NT);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = C::kSmemBytes;
   cfg.stream = st;
@@ -304,15 +311,25 @@ cudaError_t launch(const XqF8GemmArgs& a, cudaStream_t st) {
   attr[1].val.clusterDim = {(unsigned)S, 1, 1};
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, stream_kernel<NT, MATS>, map_x, p);
+  return cudaLaunchKernelEx(&cfg, stream_kernel<NT, MATS, PER_SM>, map_x, p);
+}
+
+template <int NT, int MATS>
+cudaError_t launch_nt(const XqF8GemmArgs& a, cudaStream_t st) {
+  constexpr int kMost = MATS * 16 + NT / 8 <= 34 ? 2 : 1;  // two CTAs share a multiprocessor where each has three stages
+  const xq_f8_weights* w = a.w[0];
+  const int ctas = w->Np / 128 * ((a.M + NT - 1) / NT);
+  int S = 1;
+  while (S < 8 && 2 * S * ctas <= w->sms * kMost && 4 * S <= w->Kb) S *= 2;
+  return launch<NT, MATS, kMost>(a, S, st);
 }
 
 template <int MATS>
 cudaError_t launch_mats(const XqF8GemmArgs& a, cudaStream_t st) {
-  if (a.M <= 16) return launch<16, MATS>(a, st);
-  if (a.M <= 32) return launch<32, MATS>(a, st);
-  if (a.M <= 64 || MATS == 2) return launch<64, MATS>(a, st);
-  return launch<128, MATS>(a, st);
+  if (a.M <= 16) return launch_nt<16, MATS>(a, st);
+  if (a.M <= 32) return launch_nt<32, MATS>(a, st);
+  if (a.M <= 64 || MATS == 2) return launch_nt<64, MATS>(a, st);
+  return launch_nt<MATS == 1 ? 128 : 64, MATS>(a, st);
 }
 
 }  // namespace
