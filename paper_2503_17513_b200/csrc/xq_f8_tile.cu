@@ -224,39 +224,53 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     wait_cta(drain, 0, failed, p.status);
   } else if (warp == 2) {
     // ---- scale words: this CTA's 128 token rows, and the tile's TN weight rows (both CTAs need all of them) ------------
+    // The words of four sets (16 K blocks) are requested together, so that their latency is met once.
     pdl_wait();
     bool ok = true;
-    uint32_t i = 0;
+    int e = 0;
+    uint32_t phase = 1;
+    const int sets = (p.Kb + 3) >> 2;
     for (int tile = first; tile < tiles && ok; tile += step) {
       const int tm = tile % p.tiles_m, tn = tile / p.tiles_m;
       const int row_x = tm * 256 + (int)rank * 128;
-      for (int g = 0; 4 * g < p.Kb; ++g, ++i) {
-        const int e = i % kSfRing;
-        if (i >= (uint32_t)kSfRing) {
-          ok = wait_cta(&sf_empty[e], ((i / kSfRing) - 1) & 1, failed, p.status);
-          if (!ok) break;
-        }
-        uint32_t v[4];
-        uint4* dst = reinterpret_cast<uint4*>(sf + e * C::kSfBytes);
+      for (int g = 0; g < sets && ok; g += 4) {
+        uint32_t x[4][4], w[4][C::kSfbBlocks][GATED ? 1 : 4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int m = row_x + 32 * q + lane;
-          v[q] = m < p.M ? *reinterpret_cast<const uint32_t*>(p.sx + (size_t)m * p.P + 4 * g) : 0x7F7F7F7Fu;
-        }
-        dst[lane] = make_uint4(v[0], v[1], v[2], v[3]);
+        for (int j = 0; j < 4; ++j) {
+          if (g + j < sets) {
 #pragma unroll
-        for (int h = 0; h < C::kSfbBlocks; ++h) {
+            for (int q = 0; q < 4; ++q) {
+              const int m = row_x + 32 * q + lane;
+              x[j][q] = m < p.M ? *reinterpret_cast<const uint32_t*>(p.sx + (size_t)m * p.P + 4 * (g + j)) : 0x7F7F7F7Fu;
+            }
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            // weight block of columns 128 h + 32 q .. + 31 (a tile starts at a multiple of 64)
-            const int nb = GATED ? tn : (tn * TN + 128 * h + 32 * q) >> 7;
-            v[q] = nb * 128 < p.Np ? *reinterpret_cast<const uint32_t*>(p.sw[GATED ? h : 0] + (size_t)nb * p.P + 4 * g) : 0x7F7F7F7Fu;
+            for (int h = 0; h < C::kSfbBlocks; ++h)
+#pragma unroll
+              for (int q = 0; q < (GATED ? 1 : 4); ++q) {
+                // weight block of columns 128 h + 32 q .. + 31 (a tile starts at a multiple of 64)
+                const int nb = GATED ? tn : (tn * TN + 128 * h + 32 * q) >> 7;
+                w[j][h][q] = nb * 128 < p.Np ? *reinterpret_cast<const uint32_t*>(p.sw[GATED ? h : 0] + (size_t)nb * p.P + 4 * (g + j)) : 0x7F7F7F7Fu;
+              }
           }
-          dst[32 * (1 + h) + lane] = make_uint4(v[0], v[1], v[2], v[3]);
         }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) arrive_at(xqf8::map_to(smem_u32(&sf_full[e]), 0));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (g + j < sets && ok) {
+            ok = wait_cta(&sf_empty[e], phase, failed, p.status);
+            if (ok) {
+              uint4* dst = reinterpret_cast<uint4*>(sf + e * C::kSfBytes);
+              dst[lane] = make_uint4(x[j][0], x[j][1], x[j][2], x[j][3]);
+#pragma unroll
+              for (int h = 0; h < C::kSfbBlocks; ++h)
+                dst[32 * (1 + h) + lane] = GATED ? make_uint4(w[j][h][0], w[j][h][0], w[j][h][0], w[j][h][0])
+                                                 : make_uint4(w[j][h][0], w[j][h][GATED ? 0 : 1], w[j][h][GATED ? 0 : 2], w[j][h][GATED ? 0 : 3]);
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) arrive_at(xqf8::map_to(smem_u32(&sf_full[e]), 0));
+              if (++e == kSfRing) e = 0, phase ^= 1;
+            }
+          }
+        }
       }
     }
   } else if (warp >= 4) {
