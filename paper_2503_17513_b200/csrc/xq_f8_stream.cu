@@ -28,7 +28,7 @@ struct StreamParams {
 };
 
 constexpr int kThreads = 7 * 32;
-constexpr int kSfRing = 4;  // scale words of four K blocks each, in shared memory
+constexpr int kSfRing = 5;  // sets of scale words (four K blocks each) in shared memory, one per warp that builds them
 
 // NT: token columns of a tile; MATS: 1, or 2 for the gated pair; PER_SM: CTAs that share a multiprocessor
 template <int NT, int MATS, int PER_SM>
@@ -155,44 +155,34 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
       umma_commit(acc_full);
     }
     __syncwarp();
-  } else if (warp == 2) {
+  } else {
     // ---- scale words: block 0 the tokens', then one block per weight matrix (one word: all 128 channels share it) ----
-    // The words of four sets (16 K blocks) are requested together: one after the other, their latency is longer than the MMAs.
+    // A set is a chain of latencies (loads, proxy fence, barrier) of about 900 cycles, as long as the MMAs of seven K blocks:
+    // five warps build sets in turn, each into a ring entry of its own, with the words of its next set requested ahead.
     pdl_wait();
-    int e = 0;
+    const int e = warp - 2;
+    uint32_t v[4], w[MATS];
+    auto request = [&](int g) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int m = 32 * q + lane;
+        v[q] = 32 * q < NT && m < mt ? *reinterpret_cast<const uint32_t*>(p.sx + (size_t)(t0 + m) * p.P + 4 * g) : 0x7F7F7F7Fu;
+      }
+#pragma unroll
+      for (int h = 0; h < MATS; ++h) w[h] = *reinterpret_cast<const uint32_t*>(p.sw[h] + (size_t)tile * p.P + 4 * g);
+    };
+    if (g_lo + e < g_hi) request(g_lo + e);
     uint32_t phase = 1;
-    bool ok = true;
-    for (int g = g_lo; g < g_hi && ok; g += 4) {
-      uint32_t v[4][4], w[4][MATS];
+    for (int g = g_lo + e; g < g_hi; g += kSfRing, phase ^= 1) {
+      if (!mbar_wait_bounded(&sf_empty[e], phase, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
+      uint4* dst = reinterpret_cast<uint4*>(sf + e * C::kSfBytes);
+      dst[lane] = make_uint4(v[0], v[1], v[2], v[3]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (g + j < g_hi) {
-#pragma unroll
-          for (int q = 0; q < (NT + 31) / 32; ++q) {
-            const int m = 32 * q + lane;
-            v[j][q] = m < mt ? *reinterpret_cast<const uint32_t*>(p.sx + (size_t)(t0 + m) * p.P + 4 * (g + j)) : 0x7F7F7F7Fu;
-          }
-#pragma unroll
-          for (int h = 0; h < MATS; ++h) w[j][h] = *reinterpret_cast<const uint32_t*>(p.sw[h] + (size_t)tile * p.P + 4 * (g + j));
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (g + j < g_hi && ok) {
-          ok = mbar_wait_bounded(&sf_empty[e], phase, failed, p.status, (int)XQ_ERR_TIMEOUT);
-          if (ok) {
-            uint4* dst = reinterpret_cast<uint4*>(sf + e * C::kSfBytes);
-            // rows past the token columns are never read
-            dst[lane] = make_uint4(v[j][0], v[j][NT > 32 ? 1 : 0], v[j][NT > 64 ? 2 : 0], v[j][NT > 96 ? 3 : 0]);
-#pragma unroll
-            for (int h = 0; h < MATS; ++h) dst[32 * (1 + h) + lane] = make_uint4(w[j][h], w[j][h], w[j][h], w[j][h]);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sf_full[e]);
-            if (++e == kSfRing) e = 0, phase ^= 1;
-          }
-        }
-      }
+      for (int h = 0; h < MATS; ++h) dst[32 * (1 + h) + lane] = make_uint4(w[h], w[h], w[h], w[h]);
+      if (g + kSfRing < g_hi) request(g + kSfRing);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sf_full[e]);
     }
   }
 

@@ -8,7 +8,7 @@
 // takes in 128 + TN / 2 rows per K block instead of 128 + TN, which is what keeps the operand traffic under the shared-memory
 // bandwidth.  Scales are applied by the instruction, four K blocks per scale word.
 //
-// Roles of a CTA: warp 0 loads (TMA), warp 1 issues MMAs (in the leader, rank 0, for both), warp 2 builds scale words, warps 4-11
+// Roles of a CTA: warp 0 loads (TMA), warp 1 issues MMAs (in the leader, rank 0, for both), warps 2 and 3 build scale words, warps 4-11
 // read the accumulators.  TN = 256 has one accumulator, released as soon as it is in registers; smaller tiles have two.
 #include <cuda_bf16.h>
 
@@ -38,7 +38,7 @@ struct TileCfg {
   static constexpr int kABytes = 128 * 128, kBBytes = kHalfN * 128, kStageBytes = kABytes + kBBytes;
   static constexpr int kStages = TN == 256 ? 6 : TN == 192 ? 7 : 8;
   static constexpr int kAccBufs = TN <= 224 ? 2 : 1;
-  static constexpr int kSfbBlocks = (TN + 127) / 128, kSfBytes = 512 * (1 + kSfbBlocks), kSfRing = 3;
+  static constexpr int kSfbBlocks = (TN + 127) / 128, kSfBytes = 512 * (1 + kSfbBlocks), kSfRing = 4;
   static constexpr int kSfCols = 4 * (1 + kSfbBlocks);
   static constexpr int kSfCol = kAccBufs * TN;  // two sets
   static constexpr int kOutBytes = kEpiWarps * 2048;  // a 32 x 32 bf16 box per epilogue warp
@@ -222,56 +222,53 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     pdl_launch_dependents();
     wait_cta(drain, 0, failed, p.status);
-  } else if (warp == 2) {
+  } else if (warp < 4) {
     // ---- scale words: this CTA's 128 token rows, and the tile's TN weight rows (both CTAs need all of them) ------------
-    // The words of four sets (16 K blocks) are requested together, so that their latency is met once.
+    // A set (four K blocks) is a chain of latencies of about 900 cycles: two warps build them in turn, with the words of the next
+    // one requested ahead.
     pdl_wait();
-    bool ok = true;
-    int e = 0;
-    uint32_t phase = 1;
     const int sets = (p.Kb + 3) >> 2;
-    for (int tile = first; tile < tiles && ok; tile += step) {
-      const int tm = tile % p.tiles_m, tn = tile / p.tiles_m;
-      const int row_x = tm * 256 + (int)rank * 128;
-      for (int g = 0; g < sets && ok; g += 4) {
-        uint32_t x[4][4], w[4][C::kSfbBlocks][GATED ? 1 : 4];
+    uint32_t x[4], w[C::kSfbBlocks][GATED ? 1 : 4];
+    auto request = [&](int tile, int g) {
+      const int row_x = tile % p.tiles_m * 256 + (int)rank * 128, tn = tile / p.tiles_m;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (g + j < sets) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const int m = row_x + 32 * q + lane;
-              x[j][q] = m < p.M ? *reinterpret_cast<const uint32_t*>(p.sx + (size_t)m * p.P + 4 * (g + j)) : 0x7F7F7F7Fu;
-            }
-#pragma unroll
-            for (int h = 0; h < C::kSfbBlocks; ++h)
-#pragma unroll
-              for (int q = 0; q < (GATED ? 1 : 4); ++q) {
-                // weight block of columns 128 h + 32 q .. + 31 (a tile starts at a multiple of 64)
-                const int nb = GATED ? tn : (tn * TN + 128 * h + 32 * q) >> 7;
-                w[j][h][q] = nb * 128 < p.Np ? *reinterpret_cast<const uint32_t*>(p.sw[GATED ? h : 0] + (size_t)nb * p.P + 4 * (g + j)) : 0x7F7F7F7Fu;
-              }
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (g + j < sets && ok) {
-            ok = wait_cta(&sf_empty[e], phase, failed, p.status);
-            if (ok) {
-              uint4* dst = reinterpret_cast<uint4*>(sf + e * C::kSfBytes);
-              dst[lane] = make_uint4(x[j][0], x[j][1], x[j][2], x[j][3]);
-#pragma unroll
-              for (int h = 0; h < C::kSfbBlocks; ++h)
-                dst[32 * (1 + h) + lane] = GATED ? make_uint4(w[j][h][0], w[j][h][0], w[j][h][0], w[j][h][0])
-                                                 : make_uint4(w[j][h][0], w[j][h][GATED ? 0 : 1], w[j][h][GATED ? 0 : 2], w[j][h][GATED ? 0 : 3]);
-              fence_proxy_async_smem();
-              __syncwarp();
-              if (lane == 0) arrive_at(xqf8::map_to(smem_u32(&sf_full[e]), 0));
-              if (++e == kSfRing) e = 0, phase ^= 1;
-            }
-          }
-        }
+      for (int q = 0; q < 4; ++q) {
+        const int m = row_x + 32 * q + lane;
+        x[q] = m < p.M ? *reinterpret_cast<const uint32_t*>(p.sx + (size_t)m * p.P + 4 * g) : 0x7F7F7F7Fu;
       }
+#pragma unroll
+      for (int h = 0; h < C::kSfbBlocks; ++h)
+#pragma unroll
+        for (int q = 0; q < (GATED ? 1 : 4); ++q) {
+          // weight block of columns 128 h + 32 q .. + 31 (a tile starts at a multiple of 64)
+          const int nb = GATED ? tn : (tn * TN + 128 * h + 32 * q) >> 7;
+          w[h][q] = nb * 128 < p.Np ? *reinterpret_cast<const uint32_t*>(p.sw[GATED ? h : 0] + (size_t)nb * p.P + 4 * g) : 0x7F7F7F7Fu;
+        }
+    };
+    // this warp's sets: every second one of the CTA's sequence (tile by tile), entries of the ring in order
+    int tile = first, g = warp - 2;
+    auto settle = [&] {
+      while (g >= sets && tile < tiles) g -= sets, tile += step;
+    };
+    settle();
+    if (tile < tiles) request(tile, g);
+    int e = warp - 2;
+    uint32_t phase = 1;
+    while (tile < tiles) {
+      if (!wait_cta(&sf_empty[e], phase, failed, p.status)) break;
+      uint4* dst = reinterpret_cast<uint4*>(sf + e * C::kSfBytes);
+      dst[lane] = make_uint4(x[0], x[1], x[2], x[3]);
+#pragma unroll
+      for (int h = 0; h < C::kSfbBlocks; ++h)
+        dst[32 * (1 + h) + lane] = make_uint4(w[h][0], w[h][GATED ? 0 : 1], w[h][GATED ? 0 : 2], w[h][GATED ? 0 : 3]);
+      g += 2;
+      settle();
+      if (tile < tiles) request(tile, g);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) arrive_at(xqf8::map_to(smem_u32(&sf_full[e]), 0));
+      e += 2;
+      if (e >= kSfRing) e -= kSfRing, phase ^= 1;
     }
   } else if (warp >= 4) {
     // ---- epilogue ---------------------------------------------------------------------------------------------------
