@@ -2,11 +2,11 @@
 //   out[m][n] = bf16( sum over K blocks g of 2^(ex[m][g] + ew[n / 128][g]) * sum over k in g of qx[m][k] qw[n][k] )
 // and the gated pair silu(G) * U of two such products over the same tokens.
 //
-// Bound by HBM: the weights cross once (N K bytes), the tokens are small.  128 output channels are the 128 rows of the MMA and
-// the tokens its NT columns, so that no CUDA core touches a weight byte: the 16 KiB of a 128-channel tile at one K block are one
-// bulk copy of consecutive addresses that lands as a ready operand (the weights are stored swizzled), and the tensor core applies
-// the scales of both operands (kind::mxf8f6f4).  K is cut into S slices over a cluster of S CTAs so that every multiprocessor
-// streams; the partial tiles meet in distributed shared memory, added in slice order (the result does not depend on timing).
+// Bound by HBM: the weights cross once (N K bytes), the tokens are small.  128 output channels are the rows of the MMA and
+// the tokens its NT columns, so that no CUDA core touches a weight byte: the 16 KiB of a channel tile at one K block are one bulk
+// copy of consecutive addresses that lands as a ready operand (the weights are stored swizzled), and the tensor core applies the
+// scales of both operands (kind::mxf8f6f4).  Few tiles are cut along K into S slices over a cluster of S CTAs; the partial tiles
+// meet in distributed shared memory, added in slice order (the result does not depend on timing).
 #include <cuda_bf16.h>
 
 #include "xq_f8.h"
@@ -24,36 +24,40 @@ struct StreamParams {
   __nv_bfloat16* out;    // [M, N] or null
   uint8_t *out_codes, *out_scales;
   int32_t* status;
-  int M, N, Np, Kb, P, S;
+  int M, N, Np, Kb, P;
+  int S;
 };
 
 constexpr int kThreads = 7 * 32;
-constexpr int kSfRing = 5;  // sets of scale words (four K blocks each) in shared memory, one per warp that builds them
+constexpr int kSfRing = 4;  // sets of scale words (four K blocks each) in shared memory, one per warp that builds them
+constexpr int kPiece = 128 * 128;
 
-// NT: token columns of a tile; MATS: 1, or 2 for the gated pair; PER_SM: CTAs that share a multiprocessor
-template <int NT, int MATS, int PER_SM>
+// NT: token columns of a tile; MATS: 1, or 2 for the gated pair
+template <int NT, int MATS>
 struct StreamCfg {
-  static constexpr int kStageBytes = MATS * 16384 + NT * 128;
-  static constexpr int kSfBytes = (MATS + 1) * 512;
-  static constexpr int kBudget = (PER_SM == 2 ? 113 : 226) * 1024 - 2048 - kSfRing * kSfBytes;
-  static constexpr int kStages = kBudget / kStageBytes < 12 ? kBudget / kStageBytes : 12;
+  // a stage: two pieces of the weights (two K blocks of one matrix, or one K block of both) and their tokens
+  static constexpr int kDepth = 3 - MATS, kTokenBytes = kDepth * NT * 128;
+  static constexpr int kStageBytes = 2 * kPiece + kTokenBytes;
+  static constexpr int kSfBytes = (MATS + 1) * 512, kSfCols = (MATS + 1) * 4;
   static constexpr int kRedBytes = MATS * 2048 * (NT / 4 + 7);  // partial tiles (S * ceil(NT / 4 / S) <= NT / 4 + 7 units)
   static constexpr int kAccCols = MATS * NT;
-  static constexpr int kSfCol = kAccCols;                       // two sets of (MATS + 1) * 4 columns
-  static constexpr int kNeed = kAccCols + 2 * (MATS + 1) * 4;
+  static constexpr int kNeed = kAccCols + 2 * kSfCols;
   static constexpr int kTmemCols = kNeed <= 64 ? 64 : kNeed <= 128 ? 128 : kNeed <= 256 ? 256 : 512;
-  static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kSfRing * kSfBytes + 512;
+  // scale words and barriers first, then the stages
+  static constexpr int kHead = (kSfRing * kSfBytes + 512 + 1023) / 1024 * 1024;
+  static constexpr int kStages = (227 * 1024 - 1024 - kHead) / kStageBytes;
+  static constexpr int kSmemBytes = 1024 + kHead + kStages * kStageBytes;
   static_assert(kStages >= 3 && kStages * kStageBytes >= kRedBytes, "stages hold the partial tiles");
 };
 
-template <int NT, int MATS, int PER_SM>
+template <int NT, int MATS>
 __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant__ CUtensorMap map_x, const StreamParams p) {
-  using C = StreamCfg<NT, MATS, PER_SM>;
-  constexpr int kStages = C::kStages, kStageBytes = C::kStageBytes;
+  using C = StreamCfg<NT, MATS>;
+  constexpr int kDepth = C::kDepth, kStages = C::kStages, kStageBytes = C::kStageBytes;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
-  unsigned char* base = smem_raw + (((raw + 1023u) & ~1023u) - raw);
-  unsigned char* sf = base + (size_t)kStages * kStageBytes;
+  unsigned char* sf = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  unsigned char* base = sf + C::kHead;
   uint64_t* full = reinterpret_cast<uint64_t*>(sf + kSfRing * C::kSfBytes);
   uint64_t* empty = full + kStages;
   uint64_t* sf_full = empty + kStages;
@@ -63,26 +67,28 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
   volatile int* failed = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int S = p.S, rank = blockIdx.x % S, tile = blockIdx.x / S, t0 = blockIdx.y * NT;
-  const int mt = p.M - t0 < NT ? p.M - t0 : NT;                                   // tokens of this tile
-  const int kb_lo = rank * p.Kb / S, kb_hi = (rank + 1) * p.Kb / S;               // this CTA's K blocks
-  const int nk = kb_hi - kb_lo;
-  const int g_lo = kb_lo >> 2, g_hi = (kb_hi + 3) >> 2;                           // its scale words
-
+  const int S = p.S, rank = blockIdx.x % S, n0 = blockIdx.x / S * 128, t0 = blockIdx.y * NT;
+  const int mt = p.M - t0 < NT ? p.M - t0 : NT;                         // tokens of this tile
+  const int steps = (p.Kb + kDepth - 1) / kDepth;                       // stages' worth of K blocks, cut into S slices
+  const int kb_lo = rank * steps / S * kDepth, kb_hi = min((rank + 1) * steps / S * kDepth, p.Kb);
+  const int nst = (kb_hi - kb_lo + kDepth - 1) / kDepth;                // this CTA's stages
+  const int g_lo = kb_lo >> 2, g_hi = (kb_hi + 3) >> 2;                 // its sets of scale words
   auto load_weights = [&](int kb, int s) {
     unsigned char* st = base + (size_t)s * kStageBytes;
-    mbar_expect_tx(&full[s], kStageBytes);
-#pragma unroll
-    for (int h = 0; h < MATS; ++h) bulk_g2s(st + h * 16384, p.w[h] + ((size_t)kb * p.Np + (size_t)tile * 128) * 128, 16384, &full[s]);
+    const int pieces = MATS == 2 ? 2 : min(2, kb_hi - kb);
+    mbar_expect_tx(&full[s], pieces * kPiece + C::kTokenBytes);
+    const size_t at = ((size_t)kb * p.Np + n0) * 128;
+    bulk_g2s(st, p.w[0] + at, kPiece, &full[s]);
+    if (pieces == 2) bulk_g2s(st + kPiece, MATS == 2 ? p.w[1] + at : p.w[0] + at + (size_t)p.Np * 128, kPiece, &full[s]);
   };
-  const int pre = nk < kStages ? nk : kStages;
+  const int pre = nst < kStages ? nst : kStages;
   pdl_launch_dependents();
   if (warp == 0) {
     // the weights do not depend on the kernel before this one: the first of them are under way before anything else is set up
     if (xqf8::elect_one()) {
       for (int s = 0; s < kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
       mbar_fence_init();
-      for (int i = 0; i < pre; ++i) load_weights(kb_lo + i, i);
+      for (int i = 0; i < pre; ++i) load_weights(kb_lo + i * kDepth, i);
       for (int s = 0; s < kSfRing; ++s) mbar_init(&sf_full[s], 1), mbar_init(&sf_empty[s], 1);
       mbar_init(acc_full, 1);
       *failed = 0;
@@ -103,14 +109,12 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
   if (warp == 0) {
     // ---- producer: tokens once the kernel before this one is done, then both as stages come free --------------------
     if (xqf8::elect_one()) {
-      auto load_tokens = [&](int kb, int s) {
-        tma_load_2d(base + (size_t)s * kStageBytes + MATS * 16384, &map_x, kb * 128, t0, &full[s]);
-      };
+      auto load_tokens = [&](int kb, int s) { tma_load_3d(base + (size_t)s * kStageBytes + 2 * kPiece, &map_x, 0, t0, kb, &full[s]); };
       pdl_wait();
-      for (int i = 0; i < pre; ++i) load_tokens(kb_lo + i, i);
+      for (int i = 0; i < pre; ++i) load_tokens(kb_lo + i * kDepth, i);
       int s = 0;
       uint32_t phase = 0;
-      for (int kb = kb_lo + pre; kb < kb_hi; ++kb) {
+      for (int kb = kb_lo + pre * kDepth; kb < kb_hi; kb += kDepth) {
         if (!mbar_wait_bounded(&empty[s], phase, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
         load_weights(kb, s);
         load_tokens(kb, s);
@@ -120,18 +124,18 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
     __syncwarp();
   } else if (warp == 1) {
     // ---- MMA issue ------------------------------------------------------------------------------------------
+    // (issuing takes about 20 cycles an MMA, 130 a commit and 60 a wait: hence two pieces to a stage)
     if (xqf8::elect_one()) {
       const uint64_t adesc0 = umma_desc_k128(smem_u32(base)), sfdesc0 = xqf8::sf_desc(smem_u32(sf));
       const uint32_t id0 = xqf8::idesc(128, NT, 0), id_step = xqf8::idesc(128, NT, 1) - id0;
       int s = 0, e = 0;
-      uint32_t phase = 0, sf_phase = 0, sf_set = 0, set = 0, accumulate = 0;
-      for (int kb = kb_lo; kb < kb_hi; ++kb) {
-        if (kb == kb_lo || (kb & 3) == 0) {  // the next scale words
+      uint32_t phase = 0, sf_phase = 0, set = 0, accumulate = 0;
+      uint64_t adesc = adesc0;
+      for (int kb = kb_lo; kb < kb_hi; kb += kDepth) {
+        if (kb == kb_lo || (kb & 3) == 0) {  // the next set of scale words, into the columns that the set before last used
           if (!mbar_wait_bounded(&sf_full[e], sf_phase, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
           tc_fence_after_sync();
-          // two sets of columns in turn: a copy never lands under an instruction that still reads the set before
-          set = tmem + C::kSfCol + sf_set * (MATS + 1) * 4;
-          sf_set ^= 1;
+          set = tmem + C::kAccCols + (e & 1) * C::kSfCols;
 #pragma unroll
           for (int h = 0; h <= MATS; ++h) xqf8::sf_copy<1>(set + 4 * h, sfdesc0 + (uint64_t)((e * C::kSfBytes + 512 * h) >> 4));
           umma_commit(&sf_empty[e]);
@@ -139,50 +143,59 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
         }
         if (!mbar_wait_bounded(&full[s], phase, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
         tc_fence_after_sync();
-        const uint64_t adesc = adesc0 + (uint64_t)((s * kStageBytes) >> 4), bdesc = adesc + (MATS * 16384 >> 4);
+        const uint64_t bdesc = adesc + (uint64_t)(2 * kPiece >> 4);
         const uint32_t id = id0 + (kb & 3) * id_step;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int d = 0; d < 2; ++d) {  // the two pieces
+          if (MATS == 1 && d == 1 && kb + 1 >= kb_hi) break;
 #pragma unroll
-          for (int h = 0; h < MATS; ++h)
-            xqf8::mma<1>(tmem + h * NT, adesc + (h * 16384 >> 4) + 2 * k, bdesc + 2 * k, id, accumulate, set + 4 * (1 + h), set);
-          accumulate = 1;
+          for (int k = 0; k < 4; ++k) {
+            if (MATS == 2)
+              xqf8::mma<1>(tmem + d * NT, adesc + (uint64_t)(d * kPiece >> 4) + 2 * k, bdesc + 2 * k, id, k ? 1u : accumulate, set + 4 * (1 + d), set);
+            else
+              xqf8::mma<1>(tmem, adesc + (uint64_t)(d * kPiece >> 4) + 2 * k, bdesc + (d * NT * 128 >> 4) + 2 * k, id + d * id_step,
+                           d | k ? 1u : accumulate, set + 4, set);
+          }
         }
+        accumulate = 1;
         umma_commit(&empty[s]);
-        if (++s == kStages) s = 0, phase ^= 1;
+        adesc += (uint64_t)(kStageBytes >> 4);
+        if (++s == kStages) s = 0, phase ^= 1, adesc = adesc0;
       }
       // after a failed wait this still signals once everything issued is over, so that nothing is in flight at the end
       umma_commit(acc_full);
     }
     __syncwarp();
   } else {
-    // ---- scale words: block 0 the tokens', then one block per weight matrix (one word: all 128 channels share it) ----
-    // A set is a chain of latencies (loads, proxy fence, barrier) of about 900 cycles, as long as the MMAs of seven K blocks:
-    // five warps build sets in turn, each into a ring entry of its own, with the words of its next set requested ahead.
-    pdl_wait();
-    const int e = warp - 2;
-    uint32_t v[4], w[MATS];
-    auto request = [&](int g) {
+    // ---- scale words: block 0 the tokens', then one block per weight matrix (one word: the 128 channels share it) ----
+    // A set is a chain of latencies (loads under a full memory system, proxy fence, barrier) longer than the MMAs it serves: four
+    // warps build sets in turn, each into a ring entry of its own, with the words of its next set requested ahead.
+    if (warp < 2 + kSfRing) {
+      pdl_wait();
+      const int e = warp - 2;
+      uint32_t v[4], w[MATS];
+      auto request = [&](int g) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int m = 32 * q + lane;
-        v[q] = 32 * q < NT && m < mt ? *reinterpret_cast<const uint32_t*>(p.sx + (size_t)(t0 + m) * p.P + 4 * g) : 0x7F7F7F7Fu;
+        for (int q = 0; q < 4; ++q) {
+          const int m = 32 * q + lane;
+          v[q] = 32 * q < NT && m < mt ? *reinterpret_cast<const uint32_t*>(p.sx + (size_t)(t0 + m) * p.P + 4 * g) : 0x7F7F7F7Fu;
+        }
+#pragma unroll
+        for (int h = 0; h < MATS; ++h) w[h] = *reinterpret_cast<const uint32_t*>(p.sw[h] + (size_t)(n0 >> 7) * p.P + 4 * g);
+      };
+      if (g_lo + e < g_hi) request(g_lo + e);
+      uint32_t phase = 1;
+      for (int g = g_lo + e; g < g_hi; g += kSfRing, phase ^= 1) {
+        if (!mbar_wait_bounded(&sf_empty[e], phase, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
+        uint4* dst = reinterpret_cast<uint4*>(sf + e * C::kSfBytes);
+        dst[lane] = make_uint4(v[0], v[1], v[2], v[3]);
+#pragma unroll
+        for (int h = 0; h < MATS; ++h) dst[32 * (1 + h) + lane] = make_uint4(w[h], w[h], w[h], w[h]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sf_full[e]);
+        if (g + kSfRing < g_hi) request(g + kSfRing);  // behind the fence, which waits for every load before it
       }
-#pragma unroll
-      for (int h = 0; h < MATS; ++h) w[h] = *reinterpret_cast<const uint32_t*>(p.sw[h] + (size_t)tile * p.P + 4 * g);
-    };
-    if (g_lo + e < g_hi) request(g_lo + e);
-    uint32_t phase = 1;
-    for (int g = g_lo + e; g < g_hi; g += kSfRing, phase ^= 1) {
-      if (!mbar_wait_bounded(&sf_empty[e], phase, failed, p.status, (int)XQ_ERR_TIMEOUT)) break;
-      uint4* dst = reinterpret_cast<uint4*>(sf + e * C::kSfBytes);
-      dst[lane] = make_uint4(v[0], v[1], v[2], v[3]);
-#pragma unroll
-      for (int h = 0; h < MATS; ++h) dst[32 * (1 + h) + lane] = make_uint4(w[h], w[h], w[h], w[h]);
-      if (g + kSfRing < g_hi) request(g + kSfRing);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sf_full[e]);
     }
   }
 
@@ -227,7 +240,7 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
     __syncthreads();
   }
   // ---- a warp per unit: lane = channels lane, lane + 32, lane + 64, lane + 96 of four tokens -----------------------------
-  const int n = tile * 128 + lane;
+  const int n = n0 + lane, tile = n0 >> 7;
   for (int slot = warp; slot * S + rank < units; slot += kThreads / 32) {
     const int c = 4 * (slot * S + rank);  // first token of the unit, within the tile
     float v[MATS][4][4];                  // [matrix][channel][token]
@@ -284,12 +297,22 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
   }
 }
 
-template <int NT, int MATS, int PER_SM>
-cudaError_t launch(const XqF8GemmArgs& a, int S, cudaStream_t st) {
-  using C = StreamCfg<NT, MATS, PER_SM>;
+// Tokens as [K block][row][128 bytes]: one box brings a stage's K blocks.
+bool map_tokens(CUtensorMap* map, const void* x, int M, int Kb, int box_rows, int depth) {
+  XqEncodeTiledFn enc = xq_encode_tiled_fn();
+  if (!enc) return false;
+  const cuuint64_t dims[3] = {128, (cuuint64_t)M, (cuuint64_t)Kb}, strides[2] = {(cuuint64_t)Kb * 128, 128};
+  const cuuint32_t box[3] = {128, (cuuint32_t)box_rows, (cuuint32_t)depth}, estr[3] = {1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(x), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int NT, int MATS>
+cudaError_t launch(const XqF8GemmArgs& a, cudaStream_t st) {
+  using C = StreamCfg<NT, MATS>;
   const xq_f8_weights* w = a.w[0];
   CUtensorMap map_x;
-  if (!xq_f8_map_rows(&map_x, a.codes, a.M, w->Kb * 128, NT)) return cudaErrorInvalidValue;
+  if (!map_tokens(&map_x, a.codes, a.M, w->Kb, NT, C::kDepth)) return cudaErrorInvalidValue;
   StreamParams p;
   for (int h = 0; h < 2; ++h) p.w[h] = a.w[h < MATS ? h : 0]->codes, p.sw[h] = a.w[h < MATS ? h : 0]->scales;
   p.sx = a.scales;
@@ -302,11 +325,16 @@ cudaError_t launch(const XqF8GemmArgs& a, int S, cudaStream_t st) {
   p.Np = w->Np;
   p.Kb = w->Kb;
   p.P = xq_f8_pitch(w->K);
-  p.S = S;
-  cudaError_t e = cudaFuncSetAttribute(stream_kernel<NT, MATS, PER_SM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemBytes);
+  // As many slices as leave a multiprocessor to every CTA (clusters of four at most: of 16 to 18 multiprocessors that share a
+  // cluster's network, larger ones leave some idle), each at least two stages long.  Measured in a chain of calls, one token:
+  // 14336 x 4096 20 / 12.0 / 10.9 us with 1 / 2 / 4 slices; 4096 x 6144 7.7 / 6.4 / 9.2; gated 4096 x 14336 18.8 / 23.7 with 1 / 2.
+  const int rows = (a.M + NT - 1) / NT, tiles = w->Np / 128, steps = (w->Kb + C::kDepth - 1) / C::kDepth;
+  p.S = 1;
+  while (p.S < 4 && 2LL * p.S * rows * tiles <= w->sms && 4 * p.S <= steps) p.S *= 2;
+  cudaError_t e = cudaFuncSetAttribute(stream_kernel<NT, MATS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(w->Np / 128 * S, (a.M + NT - 1) / NT);
+  cfg.gridDim = dim3(tiles * p.S, rows);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = C::kSmemBytes;
   cfg.stream = st;
@@ -314,28 +342,18 @@ cudaError_t launch(const XqF8GemmArgs& a, int S, cudaStream_t st) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim = {(unsigned)S, 1, 1};
+  attr[1].val.clusterDim = {(unsigned)p.S, 1, 1};
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, stream_kernel<NT, MATS, PER_SM>, map_x, p);
-}
-
-template <int NT, int MATS>
-cudaError_t launch_nt(const XqF8GemmArgs& a, cudaStream_t st) {
-  constexpr int kMost = MATS * 16 + NT / 8 <= 34 ? 2 : 1;  // two CTAs share a multiprocessor where each has three stages
-  const xq_f8_weights* w = a.w[0];
-  const int ctas = w->Np / 128 * ((a.M + NT - 1) / NT);
-  int S = 1;
-  while (S < 8 && 2 * S * ctas <= w->sms * kMost && 4 * S <= w->Kb) S *= 2;
-  return launch<NT, MATS, kMost>(a, S, st);
+  return cudaLaunchKernelEx(&cfg, stream_kernel<NT, MATS>, map_x, p);
 }
 
 template <int MATS>
 cudaError_t launch_mats(const XqF8GemmArgs& a, cudaStream_t st) {
-  if (a.M <= 16) return launch_nt<16, MATS>(a, st);
-  if (a.M <= 32) return launch_nt<32, MATS>(a, st);
-  if (a.M <= 64 || MATS == 2) return launch_nt<64, MATS>(a, st);
-  return launch_nt<MATS == 1 ? 128 : 64, MATS>(a, st);
+  if (a.M <= 16) return launch<16, MATS>(a, st);
+  if (a.M <= 32) return launch<32, MATS>(a, st);
+  if (a.M <= 64 || MATS == 2) return launch<64, MATS>(a, st);
+  return launch<MATS == 1 ? 128 : 64, MATS>(a, st);
 }
 
 }  // namespace

@@ -261,12 +261,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int h = 0; h < C::kSfbBlocks; ++h)
         dst[32 * (1 + h) + lane] = make_uint4(w[h][0], w[h][GATED ? 0 : 1], w[h][GATED ? 0 : 2], w[h][GATED ? 0 : 3]);
-      g += 2;
-      settle();
-      if (tile < tiles) request(tile, g);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) arrive_at(xqf8::map_to(smem_u32(&sf_full[e]), 0));
+      g += 2;
+      settle();
+      if (tile < tiles) request(tile, g);  // behind the fence, which waits for every load before it
       e += 2;
       if (e >= kSfRing) e -= kSfRing, phase ^= 1;
     }
