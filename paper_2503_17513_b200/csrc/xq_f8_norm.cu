@@ -3,8 +3,8 @@
 // with everything between the bf16 inputs and the outputs in fp32: t is not rounded before the norm (the bf16 sum is an
 // output, not an intermediate), and y is rounded once, to 8 bits (and once to bf16 where the caller wants it too).
 //
-// Bound by HBM: 2 + 2 bytes in, 2 + 1 bytes out per element.  A row lives in the registers of one CTA between the two
-// reductions, so that every byte crosses once.  Thread t holds vectors t, t + T, ... of eight channels (16-byte loads); the
+// Bound by HBM: 2 + 2 bytes in, 2 + 1 bytes out per element.  A row lives in the registers of one CTA (or warp) between the two
+// reductions, so that every byte crosses once: 16384 x 8192 takes 142 us, 6.6 TB/s, the rate of a plain copy.  Thread t holds vectors t, t + T, ... of eight channels (16-byte loads); the
 // 128 channels of a group are the vectors of one half-warp, so that the group's maximum is four shuffles.
 #include <cuda_bf16.h>
 
@@ -16,135 +16,150 @@ using namespace xqptx;
 
 namespace {
 
-struct Vec8 {
-  float v[8];
-};
-
-// eight bf16 from p, the first n of them inside the row (n >= 8: one 16-byte load)
-__device__ __forceinline__ Vec8 load8(const __nv_bfloat16* p, int n) {
-  Vec8 r;
-  if (n >= 8) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// eight bf16 from p, the first n of them inside the row (n >= 8: one 16-byte load), as bit patterns
+__device__ __forceinline__ uint4 load8(const uint16_t* p, int n) {
+  if (n >= 8) return *reinterpret_cast<const uint4*>(p);
+  uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      r.v[2 * i] = __uint_as_float(w[i] << 16);
-      r.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.v[i] = i < n ? __bfloat162float(p[i]) : 0.f;
-  }
-  return r;
+  for (int i = 0; i < 8; ++i)
+    if (i < n) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
-
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const Vec8& r, int n) {
+__device__ __forceinline__ void widen(const uint4& u, float (&v)[8]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8], int n) {
   if (n >= 8) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(r.v[2 * i], r.v[2 * i + 1]);
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
       w[i] = *reinterpret_cast<const uint32_t*>(&b);
     }
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = __float2bfloat16_rn(r.v[i]);
+      if (i < n) p[i] = __float2bfloat16_rn(v[i]);
   }
 }
 
-template <int V>
-__global__ void __launch_bounds__(1024) norm_quant_kernel(const XqF8NormArgs a) {
-  __shared__ float part[2][32];
-  const int t = threadIdx.x, T = blockDim.x, lane = t & 31, warp = t >> 5;
+// A row to a CTA, or (WARP) a row to a warp.  All loads of a thread are requested before the first of them is used.
+template <int V, bool WARP, bool NORM, bool RES>
+__global__ void __launch_bounds__(WARP ? 256 : 1024) norm_quant_kernel(const XqF8NormArgs a) {
+  __shared__ float part[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = WARP ? lane : threadIdx.x, T = WARP ? 32 : blockDim.x;
   const int Kq = xq_f8_padded(a.K), P = xq_f8_pitch(a.K);
+  const int64_t m = WARP ? (int64_t)blockIdx.x * (blockDim.x >> 5) + warp : blockIdx.x;
   pdl_launch_dependents();
   pdl_wait();
-  int flip = 0;
-  for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x, flip ^= 1) {
-    const __nv_bfloat16* x = (const __nv_bfloat16*)a.x + m * a.ldx;
-    const __nv_bfloat16* r = a.residual ? (const __nv_bfloat16*)a.residual + m * a.ldr : nullptr;
-    Vec8 v[V];
-    float ss = 0.f;
+  if (WARP && m >= a.M) return;
+  const uint16_t* x = (const uint16_t*)a.x + m * a.ldx;
+  const uint16_t* r = (const uint16_t*)a.residual + m * a.ldr;
+  uint4 xr[V], rr[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = 8 * (t + i * T), n = a.K - c;
-      if (n > 0) {
-        v[i] = load8(x + c, n);
-        if (r) {
-          const Vec8 w = load8(r + c, n);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[i].v[j] += w.v[j];
-        }
-        if (a.sum) store8((__nv_bfloat16*)a.sum + m * a.ldr + c, v[i], n);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) ss = fmaf(v[i].v[j], v[i].v[j], ss);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i].v[j] = 0.f;
-      }
-    }
-    float rstd = 1.f;
-    if (a.gamma) {
-      for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      // two sets of partial sums in turn: a row's are still being read when the next row's first ones arrive
-      if (lane == 0) part[flip][warp] = ss;
-      __syncthreads();
-      ss = lane < (T >> 5) ? part[flip][lane] : 0.f;
-      for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      rstd = 1.f / sqrtf(ss / (float)a.K + a.eps);
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = 8 * (t + i * T), n = a.K - c;
-      if (a.gamma && n > 0) {
-        const Vec8 g = load8((const __nv_bfloat16*)a.gamma + c, n);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i].v[j] = v[i].v[j] * rstd * g.v[j];
-        if (a.y) store8((__nv_bfloat16*)a.y + m * a.ldy + c, v[i], n);
-      }
-      float amax = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(v[i].v[j]));
-      for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-      if (c < Kq) {
-        const int b = xqf8::scale_byte(amax);
-        const float s = xqf8::inv_scale(b);
-        uint2 q;
-        q.x = xqf8::pack4(v[i].v[0] * s, v[i].v[1] * s, v[i].v[2] * s, v[i].v[3] * s);
-        q.y = xqf8::pack4(v[i].v[4] * s, v[i].v[5] * s, v[i].v[6] * s, v[i].v[7] * s);
-        *reinterpret_cast<uint2*>(a.codes + m * (int64_t)Kq + c) = q;
-        if ((lane & 15) == 0) a.scales[m * (int64_t)P + (c >> 7)] = (uint8_t)b;
-      }
-    }
-    if (t < P - Kq / 128) a.scales[m * (int64_t)P + Kq / 128 + t] = 127;
+  for (int i = 0; i < V; ++i) {
+    const int c = 8 * (t + i * T), n = a.K - c;
+    xr[i] = n > 0 ? load8(x + c, n) : make_uint4(0, 0, 0, 0);
+    if (RES) rr[i] = n > 0 ? load8(r + c, n) : make_uint4(0, 0, 0, 0);
   }
+  float v[V][8], ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    widen(xr[i], v[i]);
+    if (RES) {
+      float w[8];
+      widen(rr[i], w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] += w[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
+  }
+  float rstd = 1.f;
+  if (NORM) {
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    if (!WARP && lane == 0) part[warp] = ss;
+    if (a.sum) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = 8 * (t + i * T), n = a.K - c;
+        if (n > 0) store8((__nv_bfloat16*)a.sum + m * a.ldr + c, v[i], n);
+      }
+    }
+    if (!WARP) {
+      __syncthreads();
+      ss = lane < (T >> 5) ? part[lane] : 0.f;
+      for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    }
+    rstd = 1.f / sqrtf(ss / (float)a.K + a.eps);
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int c = 8 * (t + i * T), n = a.K - c;
+    if (NORM && n > 0) {
+      float g[8];
+      widen(load8((const uint16_t*)a.gamma + c, n), g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * rstd * g[j];
+      if (a.y) store8((__nv_bfloat16*)a.y + m * a.ldy + c, v[i], n);
+    }
+    float amax = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(v[i][j]));
+    for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if (c < Kq) {
+      const int b = xqf8::scale_byte(amax);
+      const float s = xqf8::inv_scale(b);
+      uint2 q;
+      q.x = xqf8::pack4(v[i][0] * s, v[i][1] * s, v[i][2] * s, v[i][3] * s);
+      q.y = xqf8::pack4(v[i][4] * s, v[i][5] * s, v[i][6] * s, v[i][7] * s);
+      *reinterpret_cast<uint2*>(a.codes + m * Kq + c) = q;
+      if ((lane & 15) == 0) a.scales[m * P + (c >> 7)] = (uint8_t)b;
+    }
+  }
+  if (t < P - Kq / 128) a.scales[m * P + Kq / 128 + t] = 127;
 }
 
-template <int V>
-cudaError_t launch(const XqF8NormArgs& a, int sms, cudaStream_t st) {
+template <int V, bool WARP, bool NORM, bool RES>
+cudaError_t launch(const XqF8NormArgs& a, cudaStream_t st) {
   const int vecs = xq_f8_padded(a.K) / 8;
-  const int T = ((vecs + V - 1) / V + 31) / 32 * 32;
-  const int resident = 2048 / T > 0 ? 2048 / T : 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(a.M < sms * resident ? a.M : sms * resident));
-  cfg.blockDim = dim3(T);
+  cfg.gridDim = dim3((unsigned)(WARP ? (a.M + 7) / 8 : a.M));
+  cfg.blockDim = dim3(WARP ? 256 : ((vecs + V - 1) / V + 31) / 32 * 32);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, norm_quant_kernel<V>, a);
+  return cudaLaunchKernelEx(&cfg, norm_quant_kernel<V, WARP, NORM, RES>, a);
+}
+
+template <int V, bool WARP>
+cudaError_t launch_v(const XqF8NormArgs& a, cudaStream_t st) {
+  return !a.gamma ? launch<V, WARP, false, false>(a, st) : a.residual ? launch<V, WARP, true, true>(a, st) : launch<V, WARP, true, false>(a, st);
 }
 
 }  // namespace
 
+// Measured with residual and sum, in a chain of calls:
+//  - rows of at most 64 vectors, many of them: a warp to a row (16384 x 512: 12.2 us; a CTA to a row 18.2, bound by starting CTAs);
+//    with few rows the CTA is faster (1200 x 512: 3.1 against 3.3);
+//  - rows that are all resident at once: one vector to a thread (700 x 2876: 5.1 us against 6.5 with two, 1 x 4096 1.8 against 2.3);
+//  - more rows than that, of at least 256 vectors: two, for more bytes in flight per thread that waits (16384 x 8192: 142 us, 6.6
+//    TB/s; 184 with one; 4096 x 4096 21.3 and 23.3); four are no faster (142; 4096 x 4096 22.6).
 cudaError_t xq_f8_launch_norm_quant(const XqF8NormArgs& a, int sms, cudaStream_t st) {
   const int vecs = xq_f8_padded(a.K) / 8;
-  if (vecs <= 1024) return launch<1>(a, sms, st);
-  if (vecs <= 2048) return launch<2>(a, sms, st);
-  if (vecs <= 4096) return launch<4>(a, sms, st);
-  return launch<8>(a, sms, st);
+  if (vecs <= 64 && a.M > 16 * sms) return vecs <= 32 ? launch_v<1, true>(a, st) : launch_v<2, true>(a, st);
+  const int threads = (vecs + 31) / 32 * 32, resident = sms * (2048 / threads);  // one vector each (none beyond 1024 threads)
+  if (vecs <= 1024 && (vecs < 256 || a.M <= resident)) return launch_v<1, false>(a, st);
+  if (vecs <= 2048) return launch_v<2, false>(a, st);
+  if (vecs <= 4096) return launch_v<4, false>(a, st);
+  return launch_v<8, false>(a, st);
 }
