@@ -94,6 +94,8 @@ struct XqF8GemmArgs {
 cudaError_t xq_f8_launch_gemm(const XqF8GemmArgs& a, cudaStream_t st);
 // its kernels: weights as the streamed operand (few tokens)
 cudaError_t xq_f8_launch_stream(const XqF8GemmArgs& a, cudaStream_t st);
+// slices that the stream kernel cuts K into: `tiles` CTAs' worth of outputs, `steps` stages along K
+int xq_f8_stream_slices(int tiles, int steps, int sms);
 // 256-token x TN-column tiles on pairs of multiprocessors (many tokens); TN 128, 192 or 256 (the gated pair: 256)
 cudaError_t xq_f8_launch_tile(const XqF8GemmArgs& a, int TN, cudaStream_t st);
 

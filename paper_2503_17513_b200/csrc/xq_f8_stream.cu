@@ -329,8 +329,7 @@ cudaError_t launch(const XqF8GemmArgs& a, cudaStream_t st) {
   // cluster's network, larger ones leave some idle), each at least two stages long.  Measured in a chain of calls, one token:
   // 14336 x 4096 20 / 12.0 / 10.9 us with 1 / 2 / 4 slices; 4096 x 6144 7.7 / 6.4 / 9.2; gated 4096 x 14336 18.8 / 23.7 with 1 / 2.
   const int rows = (a.M + NT - 1) / NT, tiles = w->Np / 128, steps = (w->Kb + C::kDepth - 1) / C::kDepth;
-  p.S = 1;
-  while (p.S < 4 && 2LL * p.S * rows * tiles <= w->sms && 4 * p.S <= steps) p.S *= 2;
+  p.S = xq_f8_stream_slices((int)((long long)rows * tiles < w->sms ? rows * tiles : w->sms), steps, w->sms);
   cudaError_t e = cudaFuncSetAttribute(stream_kernel<NT, MATS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -352,7 +351,7 @@ template <int MATS>
 cudaError_t launch_mats(const XqF8GemmArgs& a, cudaStream_t st) {
   if (a.M <= 16) return launch<16, MATS>(a, st);
   if (a.M <= 32) return launch<32, MATS>(a, st);
-  if (a.M <= 64 || MATS == 2) return launch<64, MATS>(a, st);
+  if (a.M <= 64 || MATS == 2) return launch<64, MATS>(a, st);  // (the gated pair of more tokens runs in tiles)
   return launch<MATS == 1 ? 128 : 64, MATS>(a, st);
 }
 

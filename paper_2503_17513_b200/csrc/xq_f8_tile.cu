@@ -9,7 +9,9 @@
 // bandwidth.  Scales are applied by the instruction, four K blocks per scale word.
 //
 // Roles of a CTA: warp 0 loads (TMA), warp 1 issues MMAs (in the leader, rank 0, for both), warps 2 and 3 build scale words, warps 4-11
-// read the accumulators.  TN = 256 has one accumulator, released as soon as it is in registers; smaller tiles have two.
+// read the accumulators.  There are two accumulators, so that a tile is stored while the next one is computed.  At TN = 256 tensor
+// memory has 512 columns for 2 x 256 and the 24 of the scale words: the two overlap in 24 columns, which the epilogue reads first;
+// the next tile waits for those only.
 #include <cuda_bf16.h>
 
 #include "xq_f8.h"
@@ -37,10 +39,11 @@ struct TileCfg {
   static constexpr int kHalfN = TN / 2;
   static constexpr int kABytes = 128 * 128, kBBytes = kHalfN * 128, kStageBytes = kABytes + kBBytes;
   static constexpr int kStages = TN == 256 ? 6 : TN == 192 ? 7 : 8;
-  static constexpr int kAccBufs = TN <= 224 ? 2 : 1;
+  static constexpr bool kLap = TN == 256;
   static constexpr int kSfbBlocks = (TN + 127) / 128, kSfBytes = 512 * (1 + kSfbBlocks), kSfRing = 4;
   static constexpr int kSfCols = 4 * (1 + kSfbBlocks);
-  static constexpr int kSfCol = kAccBufs * TN;  // two sets
+  static constexpr int kAccStep = kLap ? 512 - 2 * kSfCols - TN : TN;  // from one accumulator to the other
+  static constexpr int kSfCol = kAccStep + TN;                         // two sets
   static constexpr int kOutBytes = kEpiWarps * 2048;  // a 32 x 32 bf16 box per epilogue warp
   static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kOutBytes + kSfRing * kSfBytes + 512;
   static_assert(kSfCol + 2 * kSfCols <= 512, "tensor memory");
@@ -99,7 +102,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w0,
                 const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ CUtensorMap map_o, const TileParams p) {
   using C = TileCfg<TN>;
-  constexpr int kStages = C::kStages, kStageBytes = C::kStageBytes, kAccBufs = C::kAccBufs, kSfRing = C::kSfRing;
+  constexpr int kStages = C::kStages, kStageBytes = C::kStageBytes, kSfRing = C::kSfRing;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   unsigned char* base = smem_raw + (((raw + 1023u) & ~1023u) - raw);
@@ -177,11 +180,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         int s = 0, e = 0;
         uint32_t phase = 0, sf_phase = 0, sf_set = 0, tcount = 0;
         for (int tile = first; tile < tiles && ok; tile += step, ++tcount) {
-          const uint32_t buf = kAccBufs == 2 ? (tcount & 1u) : 0u, use = kAccBufs == 2 ? tcount >> 1 : tcount;
-          ok = wait_pair(&acc_empty[buf], (use & 1) ^ 1, failed, p.status);  // (the first use finds it free)
+          // (the first use finds its accumulator free; overlapping ones have one barrier, which a tile's readers pass once they are
+          // done with the tile before and with the columns that the next one overwrites)
+          const uint32_t buf = tcount & 1u;
+          ok = C::kLap ? wait_pair(&acc_empty[0], (tcount & 1) ^ 1, failed, p.status)
+                       : wait_pair(&acc_empty[buf], ((tcount >> 1) & 1) ^ 1, failed, p.status);
           if (!ok) break;
           tc_fence_after_sync();
-          const uint32_t acc = tmem + buf * TN;
+          const uint32_t acc = tmem + buf * C::kAccStep;
           uint32_t set = 0, accumulate = 0;
           for (int kb = 0; kb < p.Kb; ++kb) {
             if ((kb & 3) == 0) {
@@ -218,7 +224,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       // follow the leader tile by tile: a wait is never longer than one tile
       uint32_t tcount = 0;
       for (int tile = first; tile < tiles && ok; tile += step, ++tcount)
-        ok = wait_cta(&acc_full[kAccBufs == 2 ? tcount & 1 : 0], (kAccBufs == 2 ? tcount >> 1 : tcount) & 1, failed, p.status);
+        ok = wait_cta(&acc_full[tcount & 1], (tcount >> 1) & 1, failed, p.status);
     }
     pdl_launch_dependents();
     wait_cta(drain, 0, failed, p.status);
@@ -281,8 +287,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     for (int tile = first; tile < tiles && ok; tile += step, ++tcount) {
       const int tm = tile % p.tiles_m, tn = tile / p.tiles_m;
       const int m0 = tm * 256 + (int)rank * 128 + q * 32, m = m0 + lane;
-      const uint32_t buf = kAccBufs == 2 ? (tcount & 1u) : 0u, use = kAccBufs == 2 ? tcount >> 1 : tcount;
-      ok = wait_cta(&acc_full[buf], use & 1, failed, p.status);
+      const uint32_t buf = tcount & 1u;
+      ok = wait_cta(&acc_full[buf], (tcount >> 1) & 1, failed, p.status);
       if (GATED && !p.out) {  // the two warps that meet below go on, or stop, together
         ok_row[(tcount & 1) * 8 + warp - 4] = ok;
         bar_sync(1 + q, 64);
@@ -290,11 +296,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       tc_fence_after_sync();
-      const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + buf * TN;
+      const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + buf * C::kAccStep;
       auto release = [&] {
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) arrive_at(xqf8::map_to(smem_u32(&acc_empty[buf]), 0));
+        if (lane == 0) arrive_at(xqf8::map_to(smem_u32(&acc_empty[C::kLap ? 0 : buf]), 0));
       };
       // 32 columns of this warp's 32 rows -> the warp's box (64-byte rows, 64-byte swizzle) -> global memory
       auto store32 = [&](const float* v, int nc) {
@@ -326,24 +332,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       };
       if (!GATED) {
-        // all of the warp's columns into registers first: with one accumulator, the next tile's MMAs wait for this
-        uint32_t v[C::kHalfN / 32][32];
-#pragma unroll
-        for (int c = 0; c < C::kHalfN / 32; ++c) tmem_ld_32x32(acc + half * C::kHalfN + 32 * c, v[c]);
-        tmem_ld_wait();
-        release();
-#pragma unroll
-        for (int c = 0; c < C::kHalfN / 32; ++c)
-          store32(reinterpret_cast<const float*>(v[c]), tn * TN + half * C::kHalfN + 32 * c);
-      } else {
-        uint32_t gv[2][32], uv[2][32];
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          tmem_ld_32x32(acc + 64 * half + 32 * c, gv[c]);
-          tmem_ld_32x32(acc + 128 + 64 * half + 32 * c, uv[c]);
+        // chunks of 32 columns into registers, the one with overlapping columns (the last of the first accumulator, the first of
+        // the second) before the others
+        constexpr int kChunks = C::kHalfN / 32;
+        const int flip = C::kLap && half == 1 && buf == 0 ? kChunks - 1 : 0;  // (4 chunks: c ^ 3 reverses them)
+        uint32_t v[kChunks][32];
+        if (C::kLap) {
+          tmem_ld_32x32(acc + half * C::kHalfN + 32 * flip, v[0]);
+          if (half != (int)buf) tmem_ld_wait();
+          release();
         }
+#pragma unroll
+        for (int c = C::kLap ? 1 : 0; c < kChunks; ++c) tmem_ld_32x32(acc + half * C::kHalfN + 32 * (c ^ flip), v[c]);
         tmem_ld_wait();
-        release();
+        if (!C::kLap) release();
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+          store32(reinterpret_cast<const float*>(v[c]), tn * TN + half * C::kHalfN + 32 * (c ^ flip));
+      } else {
+        // this warp's 64 gate and 64 up columns, the chunk with overlapping columns (see above) first
+        uint32_t gv[2][32], uv[2][32];
+        const uint32_t cg = acc + 64 * half, cu = acc + 128 + 64 * half;
+        if (buf == 0) {
+          tmem_ld_32x32(cu + 32, uv[1]);
+          if (half == 1) tmem_ld_wait();
+          release();
+          tmem_ld_32x32(cg, gv[0]);
+        } else {
+          tmem_ld_32x32(cg, gv[0]);
+          if (half == 0) tmem_ld_wait();
+          release();
+          tmem_ld_32x32(cu + 32, uv[1]);
+        }
+        tmem_ld_32x32(cg + 32, gv[1]);
+        tmem_ld_32x32(cu, uv[0]);
+        tmem_ld_wait();
         float h[2][32], amax = 0.f;
 #pragma unroll
         for (int c = 0; c < 2; ++c)
