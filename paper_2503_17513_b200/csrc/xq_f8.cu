@@ -68,13 +68,6 @@ __global__ void import_kernel(const uint8_t* __restrict__ src, int N, int K, int
   }
 }
 
-__global__ void import_scales_kernel(const uint8_t* __restrict__ src, int Nb, int Kb, int P, uint8_t* __restrict__ dst) {
-  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < Nb * P; i += gridDim.x * blockDim.x) {
-    const int nb = i / P, kb = i - nb * P;
-    dst[i] = kb < Kb ? src[(size_t)nb * Kb + kb] : (uint8_t)127;
-  }
-}
-
 __global__ void export_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int N, int K, int Np, int Kb, int P,
                               uint8_t* __restrict__ out_codes, uint8_t* __restrict__ out_scales) {
   const size_t total = (size_t)N * K;
@@ -124,12 +117,13 @@ xq_status make_weights(int32_t N, int32_t K, xq_f8_weights** out) {
     delete w;
     return XQ_ERR_CUDA;
   }
-  if (cudaMalloc((void**)&w->codes, (size_t)w->Kb * w->Np * 128) != cudaSuccess ||
-      cudaMalloc((void**)&w->scales, (size_t)(w->Np / 128) * xq_f8_pitch(K)) != cudaSuccess) {
+  const size_t codes = (size_t)w->Kb * w->Np * 128;
+  if (cudaMalloc((void**)&w->codes, codes + (size_t)(w->Np / 128) * xq_f8_pitch(K)) != cudaSuccess) {
     cudaGetLastError();
-    xq_f8_weights_free(w);
+    delete w;
     return XQ_ERR_ALLOC;
   }
+  w->scales = w->codes + codes;
   *out = w;
   return XQ_OK;
 }
@@ -180,8 +174,7 @@ extern "C" {
 
 void xq_f8_weights_free(xq_f8_weights* w) {
   if (!w) return;
-  if (w->codes) cudaFree(w->codes);
-  if (w->scales) cudaFree(w->scales);
+  cudaFree(w->codes);  // (the scales lie behind the codes)
   delete w;
 }
 
@@ -232,9 +225,11 @@ xq_status xq_f8_weights_import(const uint8_t* codes, const uint8_t* scales, int3
   if (s != XQ_OK) return s;
   const int Nb = w->Np / 128;
   const size_t nc = (size_t)N * K, ns = (size_t)Nb * w->Kb;
-  std::vector<uint8_t> host;
+  const int P = xq_f8_pitch(K);
+  std::vector<uint8_t> host, rows;
   try {
     host.resize(ns);
+    rows.assign((size_t)Nb * P, 127);
   } catch (const std::bad_alloc&) {
     xq_f8_weights_free(w);
     return XQ_ERR_ALLOC;
@@ -251,21 +246,18 @@ xq_status xq_f8_weights_import(const uint8_t* codes, const uint8_t* scales, int3
     xq_f8_weights_free(w);
     return XQ_ERR_INVALID_ARG;
   }
-  DevBuf dC, dS;
+  for (int nb = 0; nb < Nb; ++nb) memcpy(&rows[(size_t)nb * P], &host[(size_t)nb * w->Kb], w->Kb);
+  DevBuf dC;
   const bool in_place = on_device(codes);
-  if ((!in_place && dC.alloc(nc) != cudaSuccess) || dS.alloc(ns) != cudaSuccess) {
+  if (!in_place && dC.alloc(nc) != cudaSuccess) {
     cudaGetLastError();
     xq_f8_weights_free(w);
     return XQ_ERR_ALLOC;
   }
-  e = cudaMemcpyAsync(dS.p, host.data(), ns, cudaMemcpyHostToDevice, st);
+  e = cudaMemcpyAsync(w->scales, rows.data(), rows.size(), cudaMemcpyHostToDevice, st);
   if (e == cudaSuccess && !in_place) e = cudaMemcpyAsync(dC.p, codes, nc, cudaMemcpyDefault, st);
   if (e == cudaSuccess) {
     import_kernel<<<w->sms * 8, 256, 0, st>>>(in_place ? codes : (const uint8_t*)dC.p, N, K, w->Np, w->Kb, w->codes);
-    e = cudaGetLastError();
-  }
-  if (e == cudaSuccess) {
-    import_scales_kernel<<<w->sms, 256, 0, st>>>((const uint8_t*)dS.p, Nb, w->Kb, xq_f8_pitch(K), w->scales);
     e = cudaGetLastError();
   }
   return finish_weights(e, w, st, out);
@@ -318,6 +310,12 @@ xq_status xq_f8_norm_quant(const void* X, int32_t M, int32_t K, int64_t ldx, con
   if (sms == 0) return XQ_ERR_CUDA;
   const XqF8NormArgs a = {X, ldx, residual_opt, ldr, gamma, eps, M, K, sum_opt, Y_opt, ldy, codes, scales};
   return status_of(xq_f8_launch_norm_quant(a, sms, (cudaStream_t)stream));
+}
+
+xq_status xq_f8_norm_quant_packed(const xq_f8_norm_quant_args* a) {
+  if (!a) return XQ_ERR_INVALID_ARG;
+  return xq_f8_norm_quant(a->X_bf16_dev, a->M, a->K, a->ldx, a->residual_bf16_opt_dev, a->ldr, a->gamma_bf16_dev, a->eps, a->sum_bf16_opt_dev,
+                          a->codes_dev, a->scales_dev, a->Y_bf16_opt_dev, a->ldy, a->stream);
 }
 
 xq_status xq_f8_gemm(const uint8_t* codes, const uint8_t* scales, int32_t M, const xq_f8_weights* w, void* out, void* ws, size_t ws_bytes,

@@ -26,7 +26,7 @@ struct xq_f8_weights {
   int32_t N, K;     // logical sizes
   int32_t Np, Kb;   // N rounded up to 128, number of K blocks
   uint8_t* codes;   // device, Kb * Np * 128
-  uint8_t* scales;  // device, (Np / 128) * P
+  uint8_t* scales;  // device, (Np / 128) * P (in the same allocation)
   int device, sms;
 };
 
