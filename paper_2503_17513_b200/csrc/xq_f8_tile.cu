@@ -146,24 +146,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
   if (warp == 0) {
     // ---- loads: this CTA's 128 token rows and its half of the weight rows ------------------------------------------
-    pdl_wait();
+    // The weights do not depend on the kernel before this one: those of the first stages are requested before the wait.
     if (xqf8::elect_one()) {
       const void* map_w = rank && GATED ? (const void*)&map_w1 : (const void*)&map_w0;
       const uint32_t full0 = xqf8::map_to(smem_u32(full), 0);  // the leader's barriers
+      auto load_weights = [&](int s, int row_w) {
+        if (rank == 0) mbar_expect_tx(&full[s], 2 * kStageBytes);  // both CTAs' copies, tokens included
+        load_pair(base + (size_t)s * kStageBytes + C::kABytes, map_w, 0, row_w, full0 + 8 * s);
+      };
+      auto first_row = [&](int tile) { return GATED ? tile / p.tiles_m * 128 : tile / p.tiles_m * TN + (int)rank * C::kHalfN; };
+      const int pre = p.Kb < kStages ? p.Kb : kStages;
+      for (int i = 0; i < pre; ++i) load_weights(i, first_row(first) + i * p.Np);
+      pdl_wait();
       bool ok = true;
       int s = 0;
       uint32_t phase = 1;  // the first pass over the ring finds it empty
       for (int tile = first; tile < tiles && ok; tile += step) {
-        const int tm = tile % p.tiles_m, tn = tile / p.tiles_m;
-        const int row_x = tm * 256 + (int)rank * 128;
-        int row_w = GATED ? tn * 128 : tn * TN + (int)rank * C::kHalfN;
+        const int row_x = tile % p.tiles_m * 256 + (int)rank * 128;
+        int row_w = first_row(tile);
         for (int kb = 0; kb < p.Kb; ++kb, row_w += p.Np) {
           ok = wait_cta(&empty[s], phase, failed, p.status);
           if (!ok) break;
-          unsigned char* st = base + (size_t)s * kStageBytes;
-          if (rank == 0) mbar_expect_tx(&full[s], 2 * kStageBytes);  // both CTAs' copies
-          load_pair(st, &map_x, kb * 128, row_x, full0 + 8 * s);
-          load_pair(st + C::kABytes, map_w, 0, row_w, full0 + 8 * s);
+          if (tile != first || kb >= pre) load_weights(s, row_w);
+          load_pair(base + (size_t)s * kStageBytes, &map_x, kb * 128, row_x, full0 + 8 * s);
           if (++s == kStages) s = 0, phase ^= 1;
         }
       }
