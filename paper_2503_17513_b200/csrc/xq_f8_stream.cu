@@ -25,7 +25,7 @@ struct StreamParams {
   uint8_t *out_codes, *out_scales;
   int32_t* status;
   int M, N, Np, Kb, P;
-  int S;
+  int S, evict_first;
 };
 
 constexpr int kThreads = 7 * 32;
@@ -73,13 +73,28 @@ __global__ void __launch_bounds__(kThreads) stream_kernel(const __grid_constant_
   const int kb_lo = rank * steps / S * kDepth, kb_hi = min((rank + 1) * steps / S * kDepth, p.Kb);
   const int nst = (kb_hi - kb_lo + kDepth - 1) / kDepth;                // this CTA's stages
   const int g_lo = kb_lo >> 2, g_hi = (kb_hi + 3) >> 2;                 // its sets of scale words
+  const uint64_t policy = l2_policy_evict_first();
+  const uint32_t first_out = p.evict_first;
+  auto load_piece = [&](unsigned char* dst, const uint8_t* src, uint64_t* bar) {
+    if (NT > 64) {  // several token tiles read the same weights
+      bulk_g2s(dst, src, kPiece, bar);
+      return;
+    }
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "@p cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;\n\t"
+        "@!p cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}" ::"r"(smem_u32(dst)),
+        "l"(src), "r"(kPiece), "r"(smem_u32(bar)), "l"(policy), "r"(first_out)
+        : "memory");
+  };
   auto load_weights = [&](int kb, int s) {
     unsigned char* st = base + (size_t)s * kStageBytes;
     const int pieces = MATS == 2 ? 2 : min(2, kb_hi - kb);
     mbar_expect_tx(&full[s], pieces * kPiece + C::kTokenBytes);
     const size_t at = ((size_t)kb * p.Np + n0) * 128;
-    bulk_g2s(st, p.w[0] + at, kPiece, &full[s]);
-    if (pieces == 2) bulk_g2s(st + kPiece, MATS == 2 ? p.w[1] + at : p.w[0] + at + (size_t)p.Np * 128, kPiece, &full[s]);
+    load_piece(st, p.w[0] + at, &full[s]);
+    if (pieces == 2) load_piece(st + kPiece, MATS == 2 ? p.w[1] + at : p.w[0] + at + (size_t)p.Np * 128, &full[s]);
   };
   const int pre = nst < kStages ? nst : kStages;
   pdl_launch_dependents();
@@ -330,6 +345,10 @@ cudaError_t launch(const XqF8GemmArgs& a, cudaStream_t st) {
   // 14336 x 4096 20 / 12.0 / 10.9 us with 1 / 2 / 4 slices; 4096 x 6144 7.7 / 6.4 / 9.2; gated 4096 x 14336 18.8 / 23.7 with 1 / 2.
   const int rows = (a.M + NT - 1) / NT, tiles = w->Np / 128, steps = (w->Kb + C::kDepth - 1) / C::kDepth;
   p.S = xq_f8_stream_slices((int)((long long)rows * tiles < w->sms ? rows * tiles : w->sms), steps, w->sms);
+  // Weights that cannot stay in the 126 MB L2 until the next pass anyway go through it first-out, so that token rows, scales and
+  // results stay (14336 x 4096, one token: 10.8 -> 10.5 us; gated 4096 x 14336 18.9 -> 18.1).  Smaller ones may be a small
+  // model's, which L2 holds whole: then plain loads are faster (4096 x 6144, 16 tokens, three of them in turn: 7.4 against 8.2 us).
+  p.evict_first = (long long)MATS * w->Np * w->Kb * 128 > 42LL << 20;
   cudaError_t e = cudaFuncSetAttribute(stream_kernel<NT, MATS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
