@@ -305,24 +305,6 @@ xq_status xq_f8_norm_quant(const void* X_bf16_dev, int32_t M, int32_t K, int64_t
                            const void* gamma_bf16_dev, float eps, void* sum_bf16_opt_dev, uint8_t* codes_dev, uint8_t* scales_dev,
                            void* Y_bf16_opt_dev, int64_t ldy, void* stream);
 
-/* The same call with its arguments in one structure, for callers that pay for every argument they pass (bindings of scripting
- * languages: a decoded token's norm takes less GPU time than such a call with fourteen arguments). */
-typedef struct {
-  const void* X_bf16_dev;
-  int64_t ldx;
-  const void* residual_bf16_opt_dev;
-  int64_t ldr;
-  const void* gamma_bf16_dev;
-  void* sum_bf16_opt_dev;
-  uint8_t *codes_dev, *scales_dev;
-  void* Y_bf16_opt_dev;
-  int64_t ldy;
-  void* stream;
-  int32_t M, K;
-  float eps;
-} xq_f8_norm_quant_args;
-xq_status xq_f8_norm_quant_packed(const xq_f8_norm_quant_args* args);
-
 /* Bytes of device workspace that xq_f8_linear needs for up to M_max tokens; xq_f8_gemm and xq_f8_gated need its first 256 only
  * (the status word).  Initialise once with xq_workspace_init; status through xq_poll_status.  Concurrent calls need distinct
  * workspaces. */

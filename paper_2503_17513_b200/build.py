@@ -1,4 +1,5 @@
-"""In-tree build of the CUDA library: nvcc for sm_100a into ``paper_2503_17513_b200/libxq.so``.
+"""In-tree build of the CUDA library: nvcc for sm_100a into ``paper_2503_17513_b200/libxq.so``, and of the small CPython
+extension ``_xq_calls.so`` beside it (host code).
 
 Run ``python -m paper_2503_17513_b200.build`` (add ``-v`` for ptxas register/shared-memory
 statistics).  nvcc cross-compiles without a GPU.
@@ -22,6 +23,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libxq.so")
 LIB_DEBUG = os.path.join(PKG, "libxq_debug.so")
+CALLS = os.path.join(PKG, "_xq_calls.so")
 
 
 def sources() -> list[str]:
@@ -39,6 +41,7 @@ def _stale(lib: str) -> bool:
 def build_library(force: bool = False, verbose: bool = False, debug_bounds: bool = False) -> str:
     """Compile every .cu to an object (in parallel, only those older than their dependencies) and link."""
     lib = LIB_DEBUG if debug_bounds else LIB
+    build_calls()
     if not force and not _stale(lib):
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
@@ -65,5 +68,23 @@ def build_library(force: bool = False, verbose: bool = False, debug_bounds: bool
     return lib
 
 
+def build_calls(force: bool = False) -> str:
+    """Compile the CPython extension with the per-token calls (host code; torch's headers and libraries)."""
+    src = os.path.join(CSRC, "xq_calls.cpp")
+    if not force and os.path.exists(CALLS) and os.path.getmtime(CALLS) >= max(os.path.getmtime(f) for f in (src, os.path.join(ROOT, "include", "xq.h"))):
+        return CALLS
+    import sysconfig
+
+    import torch
+
+    t = os.path.dirname(torch.__file__)
+    include = [os.path.join(ROOT, "include"), os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
+               os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include"), sysconfig.get_paths()["include"]]
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                    *(f"-I{d}" for d in include), src, "-o", CALLS, f"-L{t}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"], check=True)
+    return CALLS
+
+
 if __name__ == "__main__":
+    print(build_calls(force=True))
     print(build_library(force=True, verbose="-v" in sys.argv, debug_bounds="--debug-bounds" in sys.argv))

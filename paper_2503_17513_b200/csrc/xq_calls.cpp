@@ -1,0 +1,219 @@
+// The per-token calls of the 8-bit layer as a CPython extension: argument marshalling only, like the ctypes binding, but a
+// decoded token's norm takes 1.8 us on the GPU and a ctypes call with its tensor queries more than twice that on the host.
+// Tensors are read through torch's C++ interface; the entry points of libxq are called through addresses that the binding
+// hands over (bind), so that the library chosen there is the one that runs.
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include "xq.h"
+
+namespace {
+
+struct Entry {
+  decltype(&xq_f8_quant) quant;
+  decltype(&xq_f8_norm_quant) norm_quant;
+  decltype(&xq_f8_gemm) gemm;
+  decltype(&xq_f8_linear) linear;
+  decltype(&xq_f8_gated) gated;
+} g_entry;
+PyObject* g_error;  // the binding's function that raises for a status
+
+// One call's arguments by position or by name; absent ones are null.
+template <int N>
+struct Args {
+  PyObject* v[N] = {};
+  bool ok = false;
+  Args(const char* const (&names)[N], int required, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    if (n > N) {
+      PyErr_SetString(PyExc_TypeError, "too many arguments");
+      return;
+    }
+    for (Py_ssize_t i = 0; i < n; ++i) v[i] = args[i];
+    const Py_ssize_t nk = kw ? PyTuple_GET_SIZE(kw) : 0;
+    for (Py_ssize_t k = 0; k < nk; ++k) {
+      int at = 0;
+      while (at < N && PyUnicode_CompareWithASCIIString(PyTuple_GET_ITEM(kw, k), names[at]) != 0) ++at;
+      if (at == N || v[at]) {
+        PyErr_Format(PyExc_TypeError, "argument %U is unknown or given twice", PyTuple_GET_ITEM(kw, k));
+        return;
+      }
+      v[at] = args[n + k];
+    }
+    for (int i = 0; i < N; ++i) {
+      if (v[i] == Py_None) v[i] = nullptr;
+      if (!v[i] && i < required) {
+        PyErr_Format(PyExc_TypeError, "argument %s is missing", names[i]);
+        return;
+      }
+    }
+    ok = true;
+  }
+};
+
+// What is wrong with the arguments, as an AssertionError (what the binding's other calls raise).
+bool bad(const char* what) {
+  PyErr_SetString(PyExc_AssertionError, what);
+  return false;
+}
+bool tensor(PyObject* o, const at::Tensor** t) {
+  if (!THPVariable_Check(o)) return bad("expected a tensor");
+  *t = &THPVariable_Unpack(o);
+  if (!(*t)->is_cuda()) return bad("expected a CUDA tensor");
+  return true;
+}
+// a contiguous tensor of at least `bytes`
+bool flat(PyObject* o, int64_t bytes, void** p) {
+  const at::Tensor* t;
+  *p = nullptr;
+  if (!o) return true;
+  if (!tensor(o, &t)) return false;
+  if (!t->is_contiguous()) return bad("expected a contiguous tensor");
+  if ((int64_t)t->nbytes() < bytes) return bad("tensor too small");
+  *p = t->data_ptr();
+  return true;
+}
+// a 2-D tensor of 16-bit elements, [M, K] (taken from it where M < 0), rows contiguous
+bool rows(PyObject* o, int64_t* M, int64_t* K, void** p, int64_t* ld) {
+  const at::Tensor* t;
+  *p = nullptr;
+  if (!o) return true;
+  if (!tensor(o, &t)) return false;
+  if (t->dim() != 2 || t->element_size() != 2) return bad("expected 2-D rows of 16-bit elements");
+  if (*M < 0) *M = t->size(0), *K = t->size(1);
+  if (t->size(0) != *M || t->size(1) != *K || (t->stride(1) != 1 && *K > 1)) return bad("rows of another shape, or not contiguous");
+  *p = t->data_ptr();
+  *ld = t->stride(0);
+  return true;
+}
+// handle of a torch stream object, or of the current stream of the tensor's device
+bool stream_of(PyObject* stream, PyObject* t, void** st) {
+  if (!stream) {
+    *st = c10::cuda::getCurrentCUDAStream(THPVariable_Unpack(t).get_device()).stream();
+    return true;
+  }
+  PyObject* h = PyObject_GetAttrString(stream, "cuda_stream");
+  if (!h) return false;
+  *st = PyLong_AsVoidPtr(h);
+  Py_DECREF(h);
+  return !PyErr_Occurred();
+}
+// weights objects carry their C handle as ctypes' c_void_p (.handle) and their sizes (N, K)
+bool weights(PyObject* o, const xq_f8_weights** w, int64_t* N, int64_t* K) {
+  PyObject *h = PyObject_GetAttrString(o, "address"), *n = h ? PyObject_GetAttrString(o, "N") : nullptr,
+           *k = n ? PyObject_GetAttrString(o, "K") : nullptr;
+  const bool ok = k != nullptr;
+  if (ok) *w = (const xq_f8_weights*)PyLong_AsVoidPtr(h), *N = PyLong_AsLongLong(n), *K = PyLong_AsLongLong(k);
+  Py_XDECREF(h), Py_XDECREF(n), Py_XDECREF(k);
+  return ok && !PyErr_Occurred();
+}
+PyObject* done(xq_status s, const char* where) {
+  if (s == XQ_OK) Py_RETURN_NONE;
+  PyObject* r = PyObject_CallFunction(g_error, "is", (int)s, where);  // raises
+  Py_XDECREF(r);
+  return nullptr;
+}
+int64_t padded(int64_t K) { return (K + 127) / 128 * 128; }
+int64_t pitch(int64_t K) { return (K + 511) / 512 * 4; }
+
+PyObject* quant(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+  static const char* const names[] = {"X", "codes", "scales", "stream"};
+  Args<4> a(names, 3, args, n, kw);
+  int64_t M = -1, K = -1, ldx = 0;
+  void *x, *c, *s, *st;
+  if (!a.ok || !rows(a.v[0], &M, &K, &x, &ldx) || !flat(a.v[1], M * padded(K), &c) || !flat(a.v[2], M * pitch(K), &s) ||
+      !stream_of(a.v[3], a.v[0], &st))
+    return nullptr;
+  return done(g_entry.quant(x, (int32_t)M, (int32_t)K, ldx, (uint8_t*)c, (uint8_t*)s, st), "xq_f8_quant");
+}
+
+PyObject* norm_quant(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+  static const char* const names[] = {"X", "gamma", "eps", "codes", "scales", "residual", "sum_out", "y", "stream"};
+  Args<9> a(names, 5, args, n, kw);
+  int64_t M = -1, K = -1, ldx = 0, ldr = 0, lds = 0, ldy = 0;
+  void *x, *g, *c, *s, *r, *o, *y, *st;
+  if (!a.ok || !rows(a.v[0], &M, &K, &x, &ldx) || !flat(a.v[1], 2 * K, &g) || !flat(a.v[3], M * padded(K), &c) || !flat(a.v[4], M * pitch(K), &s) ||
+      !rows(a.v[5], &M, &K, &r, &ldr) || !rows(a.v[6], &M, &K, &o, &lds) || !rows(a.v[7], &M, &K, &y, &ldy) || !stream_of(a.v[8], a.v[0], &st))
+    return nullptr;
+  if (r && o && ldr != lds) return bad("residual and sum_out must have the same row pitch"), nullptr;
+  const double eps = PyFloat_AsDouble(a.v[2]);
+  if (PyErr_Occurred()) return nullptr;
+  return done(g_entry.norm_quant(x, (int32_t)M, (int32_t)K, ldx, r, r ? ldr : lds, g, (float)eps, o, (uint8_t*)c, (uint8_t*)s, y, ldy, st),
+              "xq_f8_norm_quant");
+}
+
+bool count(PyObject* o, int64_t* M) {
+  *M = PyLong_AsLongLong(o);
+  return !PyErr_Occurred();
+}
+
+PyObject* gemm(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+  static const char* const names[] = {"codes", "scales", "M", "w", "out", "ws", "stream"};
+  Args<7> a(names, 4, args, n, kw);
+  const xq_f8_weights* w;
+  int64_t M, N, K;
+  void *c, *s, *o, *ws, *st;
+  if (!a.ok || !count(a.v[2], &M) || !weights(a.v[3], &w, &N, &K) || !flat(a.v[0], M * padded(K), &c) || !flat(a.v[1], M * pitch(K), &s) ||
+      !flat(a.v[4], 2 * M * N, &o) || !flat(a.v[5], 0, &ws) || !stream_of(a.v[6], a.v[0], &st))
+    return nullptr;
+  return done(g_entry.gemm((const uint8_t*)c, (const uint8_t*)s, (int32_t)M, w, o, ws, ws ? THPVariable_Unpack(a.v[5]).nbytes() : 0, st), "xq_f8_gemm");
+}
+
+PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+  static const char* const names[] = {"X", "w", "out", "ws", "stream"};
+  Args<5> a(names, 4, args, n, kw);
+  const xq_f8_weights* w;
+  int64_t M = -1, N, K, kx = -1, ldx = 0;
+  void *x, *o, *ws, *st;
+  if (!a.ok || !weights(a.v[1], &w, &N, &K) || !rows(a.v[0], &M, &kx, &x, &ldx)) return nullptr;
+  if (kx != K) return bad("rows of another width than the weights"), nullptr;
+  if (!flat(a.v[2], 2 * M * N, &o) || !flat(a.v[3], 0, &ws) || !stream_of(a.v[4], a.v[0], &st)) return nullptr;
+  return done(g_entry.linear(x, (int32_t)M, ldx, w, o, ws, THPVariable_Unpack(a.v[3]).nbytes(), st), "xq_f8_linear");
+}
+
+PyObject* gated(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+  static const char* const names[] = {"codes", "scales", "M", "gate", "up", "ws", "out", "out_codes", "out_scales", "stream"};
+  Args<10> a(names, 6, args, n, kw);
+  const xq_f8_weights *wg, *wu;
+  int64_t M, N, K, N2, K2;
+  void *c, *s, *ws, *o, *oc, *os, *st;
+  if (!a.ok || !count(a.v[2], &M) || !weights(a.v[3], &wg, &N, &K) || !weights(a.v[4], &wu, &N2, &K2) || !flat(a.v[0], M * padded(K), &c) ||
+      !flat(a.v[1], M * pitch(K), &s) || !flat(a.v[5], 0, &ws) || !flat(a.v[6], 2 * M * N, &o) || !flat(a.v[7], M * padded(N), &oc) ||
+      !flat(a.v[8], M * pitch(N), &os) || !stream_of(a.v[9], a.v[0], &st))
+    return nullptr;
+  return done(g_entry.gated((const uint8_t*)c, (const uint8_t*)s, (int32_t)M, wg, wu, o, (uint8_t*)oc, (uint8_t*)os, ws,
+                            THPVariable_Unpack(a.v[5]).nbytes(), st),
+              "xq_f8_gated");
+}
+
+// bind(raise, quant, norm_quant, gemm, linear, gated): the function that raises and five addresses
+PyObject* bind(PyObject*, PyObject* args) {
+  PyObject* raise;
+  unsigned long long p[5];
+  if (!PyArg_ParseTuple(args, "OKKKKK", &raise, &p[0], &p[1], &p[2], &p[3], &p[4])) return nullptr;
+  Py_XDECREF(g_error);
+  Py_INCREF(raise);
+  g_error = raise;
+  g_entry.quant = (decltype(g_entry.quant))p[0];
+  g_entry.norm_quant = (decltype(g_entry.norm_quant))p[1];
+  g_entry.gemm = (decltype(g_entry.gemm))p[2];
+  g_entry.linear = (decltype(g_entry.linear))p[3];
+  g_entry.gated = (decltype(g_entry.gated))p[4];
+  Py_RETURN_NONE;
+}
+
+#define XQ_CALL(f, doc) {#f, (PyCFunction)(void*)(f), METH_FASTCALL | METH_KEYWORDS, doc}
+PyMethodDef g_methods[] = {
+    {"bind", bind, METH_VARARGS, "bind(raise, quant, norm_quant, gemm, linear, gated)"},
+    XQ_CALL(quant, "xq_f8_quant(X, codes, scales, stream=None)"),
+    XQ_CALL(norm_quant, "xq_f8_norm_quant(X, gamma, eps, codes, scales, residual=None, sum_out=None, y=None, stream=None); residual and "
+                        "sum_out may be the same tensor, and must have the same row pitch"),
+    XQ_CALL(gemm, "xq_f8_gemm(codes, scales, M, w, out, ws, stream=None)"),
+    XQ_CALL(linear, "xq_f8_linear(X, w, out, ws, stream=None)"),
+    XQ_CALL(gated, "xq_f8_gated(codes, scales, M, gate, up, ws, out=None, out_codes=None, out_scales=None, stream=None): "
+                   "silu(tokens x gate^T) * (tokens x up^T), bf16 rows into out, or 8-bit rows into out_codes and out_scales"),
+    {nullptr, nullptr, 0, nullptr}};
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_xq_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__xq_calls(void) { return PyModule_Create(&g_module); }

@@ -312,12 +312,6 @@ xq_status xq_f8_norm_quant(const void* X, int32_t M, int32_t K, int64_t ldx, con
   return status_of(xq_f8_launch_norm_quant(a, sms, (cudaStream_t)stream));
 }
 
-xq_status xq_f8_norm_quant_packed(const xq_f8_norm_quant_args* a) {
-  if (!a) return XQ_ERR_INVALID_ARG;
-  return xq_f8_norm_quant(a->X_bf16_dev, a->M, a->K, a->ldx, a->residual_bf16_opt_dev, a->ldr, a->gamma_bf16_dev, a->eps, a->sum_bf16_opt_dev,
-                          a->codes_dev, a->scales_dev, a->Y_bf16_opt_dev, a->ldy, a->stream);
-}
-
 xq_status xq_f8_gemm(const uint8_t* codes, const uint8_t* scales, int32_t M, const xq_f8_weights* w, void* out, void* ws, size_t ws_bytes,
                      void* stream) {
   XQ_RANGE();

@@ -9,7 +9,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 
 import numpy as np
 import torch
@@ -46,7 +45,7 @@ EXPORTS = [
     "xq_mx_expanded_linear_host", "xq_mx_gemm_staged", "xq_mx_rotate_quant_staged",
     "xq_mx_prepare_weights_heads", "xq_mx_weights_heads", "xq_gemm_kernel_info", "xq_selftest_i8_mma_rate", "xq_expanded_linear_host_enqueue", "xq_expanded_linear_one_launch", "xq_prepare_weights_gptq", "xq_gptq_codes",
     "xq_f8_prepare_weights", "xq_f8_weights_import", "xq_f8_weights_export", "xq_f8_weights_info", "xq_f8_weights_free", "xq_f8_quant",
-    "xq_f8_norm_quant", "xq_f8_norm_quant_packed", "xq_f8_workspace_bytes", "xq_f8_gemm", "xq_f8_linear", "xq_f8_gated",
+    "xq_f8_norm_quant", "xq_f8_workspace_bytes", "xq_f8_gemm", "xq_f8_linear", "xq_f8_gated",
 ]
 
 
@@ -119,7 +118,6 @@ def lib() -> ctypes.CDLL:
         L.xq_f8_weights_free.restype = None
         L.xq_f8_quant.argtypes = [vp, i32, i32, i64, vp, vp, vp]
         L.xq_f8_norm_quant.argtypes = [vp, i32, i32, i64, vp, i64, vp, ctypes.c_float, vp, vp, vp, vp, i64, vp]
-        L.xq_f8_norm_quant_packed.argtypes = [vp]
         L.xq_f8_workspace_bytes.argtypes = [i32, vp]
         L.xq_f8_workspace_bytes.restype = sz
         L.xq_f8_gemm.argtypes = [vp, vp, i32, vp, vp, vp, sz, vp]
@@ -480,6 +478,7 @@ class F8Weights:
 
     def __init__(self, handle: int):
         self.handle = ctypes.c_void_p(handle)
+        self.address = handle  # the same as a plain integer
         n, k = ctypes.c_int32(), ctypes.c_int32()
         _check(lib().xq_f8_weights_info(self.handle, ctypes.byref(n), ctypes.byref(k)), "xq_f8_weights_info")
         self.N, self.K = n.value, k.value
@@ -487,7 +486,7 @@ class F8Weights:
     def free(self):
         if self.handle:
             lib().xq_f8_weights_free(self.handle)
-            self.handle = ctypes.c_void_p(0)
+            self.handle, self.address = ctypes.c_void_p(0), 0
 
     def __del__(self):
         try:
@@ -555,79 +554,25 @@ def new_f8_workspace(M_max: int, w: F8Weights, device="cuda") -> torch.Tensor:
     return ws
 
 
-# The calls below are what a decoding loop makes once per layer and token, where the host's time counts: pointers go over as
-# plain integers, the stream is read by its handle, the norm's fourteen arguments travel as one structure (norm: 5 us a call
-# instead of 13 with the wrappers above, half of it the launch).
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_NORM_ARGS = struct.Struct("=QqQqQQQQQqQiifxxxx")  # xq_f8_norm_quant_args
+# xq_f8_quant, xq_f8_norm_quant, xq_f8_gemm, xq_f8_linear and xq_f8_gated are what a decoding loop calls for every layer and
+# token, where the host's time counts: they come from the extension module built beside the library (csrc/xq_calls.cpp; a norm
+# call takes 3 us with it, most of it the launch, and 13 us through ctypes).  Bound on first use, like the library.
+_NATIVE = ("quant", "norm_quant", "gemm", "linear", "gated")
 
 
-def _flat(t) -> int:
-    """Address of a contiguous device tensor."""
-    assert t.is_cuda and t.is_contiguous()
-    return t.data_ptr()
+def _raise_status(status: int, where: str):
+    raise XqError(status, where)
 
 
-def _on(stream, t) -> int:
-    """Handle of `stream`, or of the current stream of t's device."""
-    return _raw_stream(t.get_device()) if stream is None else stream.cuda_stream
-
-
-def _rows(t, shape) -> int:
-    """Row pitch of a 2-D device tensor of `shape` whose rows are contiguous."""
-    ld, step = t.stride()
-    assert t.is_cuda and t.shape == shape and (step == 1 or shape[1] == 1)
-    return ld
-
-
-def xq_f8_quant(X, codes, scales, stream=None) -> None:
-    shape = X.shape
-    M, K = shape
-    st = lib().xq_f8_quant(X.data_ptr(), M, K, _rows(X, shape), _flat(codes), _flat(scales), _on(stream, X))
-    if st:
-        raise XqError(st, "xq_f8_quant")
-
-
-def xq_f8_norm_quant(X, gamma, eps: float, codes, scales, residual=None, sum_out=None, y=None, stream=None) -> None:
-    """residual and sum_out may be the same tensor; if both are given their row pitches must be equal."""
-    shape = X.shape
-    M, K = shape
-    rp = sp = yp = ldr = ldy = 0
-    if residual is not None:
-        ldr, rp = _rows(residual, shape), residual.data_ptr()
-    if sum_out is not None:
-        if sum_out is not residual:
-            lds = _rows(sum_out, shape)
-            assert residual is None or lds == ldr
-            ldr = lds
-        sp = sum_out.data_ptr()
-    if y is not None:
-        ldy, yp = _rows(y, shape), y.data_ptr()
-    assert gamma.numel() == K
-    args = _NORM_ARGS.pack(X.data_ptr(), _rows(X, shape), rp, ldr, _flat(gamma), sp, _flat(codes), _flat(scales), yp, ldy, _on(stream, X), M, K, eps)
-    st = lib().xq_f8_norm_quant_packed(args)
-    if st:
-        raise XqError(st, "xq_f8_norm_quant")
-
-
-def xq_f8_gemm(codes, scales, M: int, w: F8Weights, out, ws, stream=None) -> None:
-    st = lib().xq_f8_gemm(_flat(codes), _flat(scales), M, w.handle, None if out is None else _flat(out), _flat(ws), ws.nbytes, _on(stream, ws))
-    if st:
-        raise XqError(st, "xq_f8_gemm")
-
-
-def xq_f8_linear(X, w: F8Weights, out, ws, M=None, ldx=None, stream=None) -> None:
-    M = X.shape[0] if M is None else M
-    ldx = X.stride(0) if ldx is None else ldx
-    st = lib().xq_f8_linear(X.data_ptr(), M, ldx, w.handle, _flat(out), _flat(ws), ws.nbytes, _on(stream, ws))
-    if st:
-        raise XqError(st, "xq_f8_linear")
-
-
-def xq_f8_gated(codes, scales, M: int, gate: F8Weights, up: F8Weights, ws, out=None, out_codes=None, out_scales=None, stream=None) -> None:
-    """silu(tokens x gate^T) * (tokens x up^T): bf16 rows into `out`, or 8-bit rows into `out_codes` and `out_scales`."""
-    st = lib().xq_f8_gated(_flat(codes), _flat(scales), M, gate.handle, up.handle, None if out is None else _flat(out),
-                           None if out_codes is None else _flat(out_codes), None if out_scales is None else _flat(out_scales), _flat(ws),
-                           ws.nbytes, _on(stream, ws))
-    if st:
-        raise XqError(st, "xq_f8_gated")
+def __getattr__(name):
+    if name.startswith("xq_f8_") and name[6:] in _NATIVE:
+        L = lib()
+        try:
+            from . import _xq_calls
+        except ImportError as e:
+            raise RuntimeError(f"{_PKG}/_xq_calls.so is missing: build it with `python -m paper_2503_17513_b200.build`") from e
+        _xq_calls.bind(_raise_status, *(ctypes.cast(getattr(L, "xq_f8_" + n), ctypes.c_void_p).value for n in _NATIVE))
+        for n in _NATIVE:
+            globals()["xq_f8_" + n] = getattr(_xq_calls, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -35,8 +35,6 @@ def test_null_and_bad_arguments_rejected_before_any_cuda_call(xq):
     assert L.xq_f8_norm_quant(null, 0, 8, 8, null, 0, null, 1e-5, null, null, null, null, 0, null) == xq.OK
     assert L.xq_f8_norm_quant(some, 4, 8, 8, null, 0, some, -1.0, null, some, some, null, 0, null) == bad
     assert L.xq_f8_norm_quant(some, 4, 8, 8, some, 4, some, 1e-5, null, some, some, null, 0, null) == bad  # residual pitch
-    assert L.xq_f8_norm_quant_packed(null) == bad
-    assert L.xq_f8_norm_quant_packed(b"\0" * 128) == bad  # K = 0
     assert L.xq_f8_gemm(null, null, 4, null, null, null, 0, null) == bad
     assert L.xq_f8_linear(null, 4, 8, null, null, null, 0, null) == bad
     assert L.xq_f8_gated(null, null, 4, null, null, null, null, null, null, 0, null) == bad
@@ -48,19 +46,24 @@ def test_sizes(xq):
     assert [xq.f8_scale_pitch(k) for k in (1, 128, 512, 513, 4096)] == [4, 4, 4, 8, 32]
 
 
-def test_packed_arguments_have_the_c_layout(xq, tmp_path):
-    """The binding's structure format against the header's, by the C compiler's offsets."""
-    import os
-    import subprocess
+def test_native_calls_check_their_arguments(xq):
+    """Wrong names, kinds and places of arguments are Python errors, raised before anything reaches the library."""
+    import torch
 
-    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    src = tmp_path / "l.c"
-    fields = ["X_bf16_dev", "ldx", "residual_bf16_opt_dev", "ldr", "gamma_bf16_dev", "sum_bf16_opt_dev", "codes_dev", "scales_dev", "Y_bf16_opt_dev",
-              "ldy", "stream", "M", "K", "eps"]
-    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "xq.h"\nint main(void) {'
-                   + "".join(f'printf("%zu ", offsetof(xq_f8_norm_quant_args, {f}));' for f in fields)
-                   + 'printf("%zu", sizeof(xq_f8_norm_quant_args)); return 0; }')
-    exe = tmp_path / "l"
-    subprocess.run(["gcc", "-I", os.path.join(root, "include"), str(src), "-o", str(exe)], check=True)
-    got = [int(v) for v in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
-    assert got == [8 * i for i in range(11)] + [88, 92, 96, 104] and xq._NORM_ARGS.size == 104
+    X, c = torch.zeros((2, 8), dtype=torch.bfloat16), torch.zeros((2, 128), dtype=torch.uint8)
+    with pytest.raises(TypeError):
+        xq.xq_f8_quant(X, c)
+    with pytest.raises(TypeError):
+        xq.xq_f8_quant(X, c, c, nonsense=1)
+    with pytest.raises(TypeError):
+        xq.xq_f8_quant(X, c, c, codes=c)
+    with pytest.raises(TypeError):
+        xq.xq_f8_quant(X, c, c, None, None)
+    with pytest.raises(AssertionError):
+        xq.xq_f8_quant(X, c, c)  # not on a GPU
+    with pytest.raises(AssertionError):
+        xq.xq_f8_quant(3, c, c)
+    with pytest.raises(AttributeError):
+        xq.xq_f8_gemm(c, c, 2, X, c, c)  # no weights object
+    with pytest.raises(AttributeError):
+        xq.no_such_call
