@@ -58,8 +58,9 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
   const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
   return lo | (hi << 16);
 }
-// silu(g) * u.  The fast exponential and quotient are within 2^-20 relative where the result matters for a sum of magnitude 1
-// (|g| < 8) and within |g| 2^-23 below, far under the 2^-9 of the rounding that follows.
+// silu(g) * u.  The fast exponential and quotient are off by about (|g| + 8) 2^-23 relative for negative g (the error of the
+// exponent, less for positive g): far under the rounding that follows (2^-9), and at large |g|, where it grows, under what the
+// fp32 sum g itself is off by.
 __device__ __forceinline__ float silu_mul(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
 
 }  // namespace xqf8

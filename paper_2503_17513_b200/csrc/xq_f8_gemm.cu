@@ -35,6 +35,7 @@ cudaError_t xq_f8_launch_gemm(const XqF8GemmArgs& a, cudaStream_t st) {
   const long long sms = w->sms, Kb = w->Kb, ctas = up(w->N, 128) * up(a.M, 128);
   const long long S = xq_f8_stream_slices((int)(ctas < sms ? ctas : sms), (int)up(Kb, 2), w->sms);
   double best = 150 + up(ctas * S, sms) * (270 + 29.5 * up(Kb, S));
+  if (up(a.M, 128) > 65535) best = 1e30;  // (the token tiles of the stream kernel are its grid's second dimension)
   int choice = 0;
   const double c[3] = {27, 21.6, 20.5};
   const int TN[3] = {256, 192, 128};
