@@ -4,8 +4,9 @@
 // output, not an intermediate), and y is rounded once, to 8 bits (and once to bf16 where the caller wants it too).
 //
 // Bound by HBM: 2 + 2 bytes in, 2 + 1 bytes out per element.  A row lives in the registers of one CTA (or warp) between the two
-// reductions, so that every byte crosses once: 16384 x 8192 takes 142 us, 6.6 TB/s, the rate of a plain copy.  Thread t holds vectors t, t + T, ... of eight channels (16-byte loads); the
-// 128 channels of a group are the vectors of one half-warp, so that the group's maximum is four shuffles.
+// reductions, so that every byte crosses once: 16384 x 8192 takes 142 us, 6.6 TB/s, the rate of a plain copy.
+// Thread t holds vectors t, t + T, ... of eight channels (16-byte loads); the 128 channels of a group are the vectors of one
+// half-warp, so that the group's maximum is four shuffles.
 #include <cuda_bf16.h>
 
 #include "xq_f8.h"
