@@ -267,6 +267,15 @@ def test_gemm(xq, M, K, N):
     assert_bf16_within(np64(out), want, err)
 
 
+# sizes that run in tiles of 256, 192 and 128 columns, over several waves of tiles, with rows that do and do not start on 16 bytes
+TILE_SIZES = [(3000, 640, 4000), (2500, 300, 6001), (2100, 1152, 4168), (2000, 900, 5003), (512, 4096, 4096), (600, 4096, 2001)]
+
+
+@pytest.mark.parametrize("M,K,N", TILE_SIZES)
+def test_gemm_in_tiles(xq, M, K, N):
+    test_gemm(xq, M, K, N)
+
+
 def gated_want(x, g, u):
     G, eG = product(x, g)
     Uu, eU = product(x, u)
@@ -294,6 +303,12 @@ def test_gated(xq, M, K, N, eight):
         xq.xq_f8_gated(cuda(xc), cuda(xs), M, hg, hu, ws, out=out)
         assert xq.xq_poll_status(ws) == xq.OK
         assert_bf16_within(np64(out), want, err)
+
+
+@pytest.mark.parametrize("M,K,N", [(1500, 256, 4000), (700, 1100, 5003)])
+@pytest.mark.parametrize("eight", [False, True])
+def test_gated_over_several_waves(xq, M, K, N, eight):
+    test_gated(xq, M, K, N, eight)
 
 
 def test_gated_large_gates(xq):
@@ -417,6 +432,28 @@ def test_repeated_launches_and_a_chain(xq, M):
     assert xq.xq_poll_status(ws, side) == xq.OK and xq.xq_poll_status(wsd, side) == xq.OK
     for r in got:
         assert all(torch.equal(a, b) for a, b in zip(r, ref))
+
+
+@pytest.mark.parametrize("M,K,N,times", [(16, 4096, 6144, 300), (1, 14336, 2048, 200), (120, 2048, 4096, 200), (2048, 2048, 4096, 60), (768, 2048, 4000, 60)])
+def test_products_repeat_bit_for_bit(xq, M, K, N, times):
+    """Back-to-back launches under load: a stage handed over too early would change some of the outputs some of the time."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    codes = torch.randint(0, 127, (M, K), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(115, 130, (M, f8.pitch(K)), generator=g, device="cuda", dtype=torch.uint8)
+    wc = torch.randint(0, 127, (N, K), generator=g, device="cuda", dtype=torch.uint8)
+    wc |= torch.randint(0, 2, (N, K), generator=g, device="cuda", dtype=torch.uint8) << 7
+    h = xq.xq_f8_weights_import(wc, torch.randint(115, 130, (-(-N // 128), -(-K // 128)), generator=g, device="cuda", dtype=torch.uint8))
+    ws = xq.new_f8_workspace(M, h)
+    ref, out = (torch.empty((M, N), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    xq.xq_f8_gemm(codes, scales, M, h, ref, ws)
+    differ = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(times // 4):
+        for _ in range(3):
+            xq.xq_f8_gemm(codes, scales, M, h, out, ws)
+        out.fill_(float("nan"))
+        xq.xq_f8_gemm(codes, scales, M, h, out, ws)
+        differ += (out != ref).sum()
+    assert int(differ) == 0 and xq.xq_poll_status(ws) == xq.OK
 
 
 def test_layers_on_distinct_streams(xq):
