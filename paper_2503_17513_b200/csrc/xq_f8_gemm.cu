@@ -13,34 +13,39 @@ bool xq_f8_map_rows(CUtensorMap* map, const void* p, int rows, int pitch, int bo
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// As many slices as leave a multiprocessor to every CTA, each at least two stages long (one stage: no gain, 16 tokens of a gated
+// 1024 x 1024 4.7 -> 5.1 us).  A cluster's CTAs share one of the chip's groups of 16 to 18 multiprocessors, so clusters of eight fill at
+// most two of them in each group: only up to three quarters of the chip.  Measured in a chain of calls, one token: 14336 x 4096 20 /
+// 12.0 / 10.9 us with 1 / 2 / 4 slices; 4096 x 6144 7.7 / 6.4 / 9.2; gated 4096 x 14336 18.8 / 23.7 with 1 / 2; 14336 x 1024 7.1 / 5.9 with 4 / 8.
 int xq_f8_stream_slices(int tiles, int steps, int sms) {
   int S = 1;
-  while (S < 4 && 2LL * S * tiles <= sms && 4 * S <= steps) S *= 2;
+  while (S < 8 && 2LL * S * tiles <= (S < 4 ? sms : sms * 3 / 4) && 4 * S <= steps) S *= 2;
   return S;
 }
 
-// Up to 64 tokens the weights are streamed.  Measured in a chain of calls, stream against 256-column tiles: gated pair 4096 x 14336
-// 64 tokens 24.0 / 29.7 us, 128 tokens 43.8 / 31.1; 2048 x 8192 64 tokens 11.7 / 12.2, 100 tokens 13.2 / 12.5.  Above, one product
-// takes the kernel and tile width with the shortest estimate, in units of 0.01 us:
-//  - stream with 128 token columns: 150 + waves of CTAs * (270 + 29.5 per K block of its slice);
+// Up to 64 tokens the weights are streamed.  Above, the kernel and tile width with the shortest estimate, in units of 0.01 us:
+//  - stream, tiles of 128 token columns (gated pair: 64): 150 + waves of CTAs * (270 + 29.5 (58) per K block of a CTA's slice);
 //  - tiles: 650 + waves of pairs * (30 + c per K block), c = 20.5, 21.6 and 27 for 128, 192 and 256 columns (narrow tiles are bound by
 //    the operands' way into shared memory).
-// Measured (us, stream / 128 / 192 / 256 columns): 333 tokens x 2720 x 5008 11.0 / 14.8 / 11.2 / 13.3; 512 x 4096 x 4096 13.7 / 12.5 /
-// 13.9 / 15.5; 768 x 4096 x 4096 - / 19.1 / 15.4 / 17.7; 256 x 14336 x 4096 20.8 / 28.4 / 30.0 / 37.8; 4096 x 14336 x 4096 - / 234 / 205 / 200.
+// Measured in a chain of calls (us, stream / 128 / 192 / 256 columns): 333 tokens x 2720 x 5008 11.0 / 14.8 / 11.2 / 13.3; 512 x 4096 x 4096
+// 13.7 / 12.5 / 13.9 / 15.5; 768 x 4096 x 4096 - / 19.1 / 15.4 / 17.7; 256 x 14336 x 4096 20.8 / 28.4 / 30.0 / 37.8; 4096 x 14336 x 4096
+// - / 234 / 205 / 200.  Gated (stream / 256): 64 tokens 4096 x 14336 24.0 / 29.7, 128 tokens 43.8 / 31.1; 100 x 2048 x 8192 13.2 / 12.5;
+// 200 x 14000 x 256 10.5 / 36.9.
 cudaError_t xq_f8_launch_gemm(const XqF8GemmArgs& a, cudaStream_t st) {
   const xq_f8_weights* w = a.w[0];
   if (a.M <= 64) return xq_f8_launch_stream(a, st);
-  if (a.w[1]) return xq_f8_launch_tile(a, 256, st);
   auto up = [](long long v, long long d) { return (v + d - 1) / d; };
-  const long long sms = w->sms, Kb = w->Kb, ctas = up(w->N, 128) * up(a.M, 128);
-  const long long S = xq_f8_stream_slices((int)(ctas < sms ? ctas : sms), (int)up(Kb, 2), w->sms);
-  double best = 150 + up(ctas * S, sms) * (270 + 29.5 * up(Kb, S));
-  if (up(a.M, 128) > 65535) best = 1e30;  // (the token tiles of the stream kernel are its grid's second dimension)
+  const bool gated = a.w[1] != nullptr;
+  const int NT = gated ? 64 : 128;  // token columns of the stream kernel
+  const long long sms = w->sms, Kb = w->Kb, ctas = up(w->N, 128) * up(a.M, NT);
+  const long long S = xq_f8_stream_slices((int)(ctas < sms ? ctas : sms), (int)(gated ? Kb : up(Kb, 2)), w->sms);
+  double best = 150 + up(ctas * S, sms) * (270 + (gated ? 58 : 29.5) * up(Kb, S));
+  if (up(a.M, NT) > 65535) best = 1e30;  // (the token tiles of the stream kernel are its grid's second dimension)
   int choice = 0;
   const double c[3] = {27, 21.6, 20.5};
   const int TN[3] = {256, 192, 128};
-  for (int i = 0; i < 3; ++i) {
-    const double t = 650 + up(up(a.M, 256) * up(w->N, TN[i]), sms / 2) * (30 + c[i] * Kb);
+  for (int i = 0; i < (gated ? 1 : 3); ++i) {
+    const double t = 650 + up(up(a.M, 256) * up(w->N, gated ? 128 : TN[i]), sms / 2) * (30 + c[i] * Kb);
     if (t < best) best = t, choice = TN[i];
   }
   return choice ? xq_f8_launch_tile(a, choice, st) : xq_f8_launch_stream(a, st);

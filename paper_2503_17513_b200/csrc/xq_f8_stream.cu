@@ -344,9 +344,6 @@ cudaError_t launch(const XqF8GemmArgs& a, cudaStream_t st) {
   p.Np = w->Np;
   p.Kb = w->Kb;
   p.P = xq_f8_pitch(w->K);
-  // As many slices as leave a multiprocessor to every CTA (clusters of four at most: of 16 to 18 multiprocessors that share a
-  // cluster's network, larger ones leave some idle), each at least two stages long.  Measured in a chain of calls, one token:
-  // 14336 x 4096 20 / 12.0 / 10.9 us with 1 / 2 / 4 slices; 4096 x 6144 7.7 / 6.4 / 9.2; gated 4096 x 14336 18.8 / 23.7 with 1 / 2.
   const int rows = (a.M + NT - 1) / NT, tiles = w->Np / 128, steps = (w->Kb + C::kDepth - 1) / C::kDepth;
   p.S = xq_f8_stream_slices((int)((long long)rows * tiles < w->sms ? rows * tiles : w->sms), steps, w->sms);
   // Weights that cannot stay in the 126 MB L2 until the next pass anyway go through it first-out, so that token rows, scales and
@@ -374,7 +371,7 @@ template <int MATS>
 cudaError_t launch_mats(const XqF8GemmArgs& a, cudaStream_t st) {
   if (a.M <= 16) return launch<16, MATS>(a, st);
   if (a.M <= 32) return launch<32, MATS>(a, st);
-  if (a.M <= 64 || MATS == 2) return launch<64, MATS>(a, st);  // (the gated pair of more tokens runs in tiles)
+  if (a.M <= 64 || MATS == 2) return launch<64, MATS>(a, st);
   return launch<MATS == 1 ? 128 : 64, MATS>(a, st);
 }
 

@@ -268,11 +268,12 @@ def test_gemm(xq, M, K, N):
 
 
 # sizes that run in tiles of 256, 192 and 128 columns, over several waves of tiles, with rows that do and do not start on 16 bytes
+SLICED_SIZES = [(1, 14336, 256), (40, 9000, 130), (200, 14000, 256)]  # few tiles, K cut into eight slices
 TILE_SIZES = [(3000, 640, 4000), (2500, 300, 6001), (2100, 1152, 4168), (2000, 900, 5003), (512, 4096, 4096), (600, 4096, 2001)]
 
 
-@pytest.mark.parametrize("M,K,N", TILE_SIZES)
-def test_gemm_in_tiles(xq, M, K, N):
+@pytest.mark.parametrize("M,K,N", TILE_SIZES + SLICED_SIZES)
+def test_gemm_tiles_and_slices(xq, M, K, N):
     test_gemm(xq, M, K, N)
 
 
@@ -305,9 +306,9 @@ def test_gated(xq, M, K, N, eight):
         assert_bf16_within(np64(out), want, err)
 
 
-@pytest.mark.parametrize("M,K,N", [(1500, 256, 4000), (700, 1100, 5003)])
+@pytest.mark.parametrize("M,K,N", [(1500, 256, 4000), (700, 1100, 5003)] + SLICED_SIZES)
 @pytest.mark.parametrize("eight", [False, True])
-def test_gated_over_several_waves(xq, M, K, N, eight):
+def test_gated_tiles_and_slices(xq, M, K, N, eight):
     test_gated(xq, M, K, N, eight)
 
 
